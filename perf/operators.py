@@ -47,7 +47,7 @@ def listed():
         # a training pass of the headline workload's size, states kept as often as is fastest
         _scan("scan_train_bf16", "train", "bf16", 64, 1000, 1024, 16, spacing=8),
         # a training pass over long sequences that keeps few states, in float32 and batch-major
-        _scan("scan_train_fp32_lean", "train", "fp32", 4, 2000, 512, 16, spacing=64, layout="batch"),
+        _scan("scan_train_fp32_lean", "train", "fp32", 4, 2000, 512, 16, spacing=32, layout="batch"),
         # a short ragged batch with nothing a multiple of eight, continued from kept states
         _scan("scan_train_bf16_ragged", "train", "bf16", 13, 161, 300, 10, groups=2, spacing=16, ragged=True, state=True),
         # a small vocabulary, exact float32, some rows masked: evaluation only
@@ -91,7 +91,7 @@ def draw(rng):
             channels = max(groups, channels - channels % groups)
             while batch * t * channels * states > 500_000_000:
                 t = t * 3 // 4
-            c = _scan(None, do, dtype, batch, max(1, t), channels, states, groups, rng.choice((8, 8, 16, 32, 64)),
+            c = _scan(None, do, dtype, batch, max(1, t), channels, states, groups, rng.choice((8, 8, 16, 32)),
                       gate=rng.random() < 0.8, **more)
     del c["name"]
     return c
