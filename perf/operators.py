@@ -194,7 +194,7 @@ def _prepare_distill(c, dev, g):
         short = torch.randint(1, K + 1, (R, 1), generator=g, device=dev)            # fewer entries than there is room for
         s["indices"][torch.arange(K, device=dev)[None] >= short] = -1
     s["dloss"] = torch.ones(1, device=dev)
-    s["loss"], s["row_loss"], s["row_lse"] = (torch.zeros(n, device=dev) for n in (1, R, R))
+    s["loss"], s["row_loss"], s["row_stats"] = (torch.zeros(n, device=dev) for n in (1, R, 2 * R))
     s["dlogits"] = torch.zeros_like(s["logits"]) if c["do"] == "train" else None
     return s
 
@@ -260,7 +260,7 @@ def _own_distill(s):
                                    s["row_loss"], s["dlogits"])
     else:
         B.mebptt_distill_loss(s["desc"], s["logits"], s["indices"], s["values"], s["weights"], stream, s["loss"], s["row_loss"],
-                              s["row_lse"])
+                              s["row_stats"])
     return _outputs(c, s)
 
 
