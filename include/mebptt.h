@@ -470,6 +470,155 @@ int mebptt_gemm_bf16(const void *A, int64_t lda, int a_major, const void *B, int
                      float *C, int64_t ldc, int accumulate, const float *bias,
                      int64_t M, int64_t N, int64_t K, int *status, void *stream);
 
+/* ---- operators over sequences ------------------------------------------------------ */
+/*
+ * What a recurrent language model has around and in place of the cores above: a short causal
+ * convolution, a selective state space scan (a recurrent core whose state is decayed and fed by
+ * amounts that depend on the input), and the loss of a student that learns from a teacher's most
+ * likely tokens.  (The paper has no counterpart; the scan's backward pass is its subject: states are
+ * kept every few steps -- equal cuts, Section 2.2 -- and recomputed between them.)
+ *
+ * Conventions of this group, next to those of the whole file
+ *   - "operand type" is bfloat16 under MEBPTT_BF16, float32 under MEBPTT_FP32 and MEBPTT_TF32 (the
+ *     same thing here); everything is computed in float32 and rounded once where it is stored.
+ *   - An array [t][B][width] over time has strides: the element of step k, row b and column i lies at
+ *     k * step + b * row + i.  step = row = 0 stands for a dense array, time-major.  Columns are
+ *     contiguous; steps and rows may come in either order and with gaps (batch-major arrays, column
+ *     slices of a wider one), but no two elements may share a place: MEBPTT_ERR_ARG otherwise.  The
+ *     gradient of an array has that array's strides.  Any alignment that the type allows is right;
+ *     columns that come in groups of eight on 16-byte boundaries are fastest.
+ *   - lengths (nullable): int32 [B] on the device; row b has lengths[b] steps, 0 to t (other values
+ *     are taken as the nearest of these).  What lies at later steps is not read; outputs and
+ *     gradients of the operand type there are written as zeros.  NULL: every row has t steps.
+ *   - States are those before the first step (s_in, nullable: zeros) and after a row's last one
+ *     (s_out, nullable: not wanted).  A row of no steps hands s_in on.  s_out may be s_in itself: so a
+ *     program generates token by token, with t = 1.  ds_out (nullable: zeros) is the gradient of
+ *     s_out, ds_in (nullable) that of s_in.
+ *   - Outputs are overwritten, not accumulated, and apart from s_out none may overlap an input.
+ *     No atomics: the same inputs give the same bits.
+ *   - Kernels only, on `stream` alone, with nothing allocated and nothing kept between calls: every
+ *     call can be captured into a graph.  Calls whose work may overlap need workspaces of their own.
+ */
+
+/*
+ * Short causal convolution, each channel by itself:
+ *     p_k = bias + sum_{j = 0}^{width-1} w[j] x_{k - width + 1 + j},   y_k = silu(p_k) or p_k.
+ * x at negative k comes from the state, the last width - 1 inputs, oldest first.
+ *   x, y [t][B][D] operand type; w [D][width] operand type, bias [D] float32 (nullable);
+ *   states and their gradients [B][width - 1][D], operand type; dw, dbias float32.
+ * 1 <= width <= 8 (a width of 1 has no state: state pointers are ignored).
+ */
+enum { MEBPTT_CONV_SILU = 1 };
+typedef struct {
+  int32_t batch, channels, width;
+  int32_t dtype;
+  int32_t flags;               /* MEBPTT_CONV_SILU or 0 */
+  int32_t reserved;            /* 0 */
+  int64_t t;
+  int64_t x_step, x_row;       /* of x and dx */
+  int64_t y_step, y_row;       /* of y and dy */
+} mebptt_conv_desc;
+
+int mebptt_conv_forward(const mebptt_conv_desc *desc, const void *x, const void *w, const float *bias,
+                        const void *s_in, const int32_t *lengths, void *stream, void *y, void *s_out);
+/* Device workspace of mebptt_conv_backward; 0 on a bad descriptor. */
+size_t mebptt_conv_workspace_bytes(const mebptt_conv_desc *desc);
+/* dbias may be NULL; s_in is the state that the forward call began with (not what it may since have been
+ * overwritten with). */
+int mebptt_conv_backward(const mebptt_conv_desc *desc, const void *x, const void *w, const float *bias,
+                         const void *s_in, const int32_t *lengths, const void *dy, const void *ds_out,
+                         void *workspace, size_t workspace_bytes, void *stream,
+                         void *dx, float *dw, float *dbias, void *ds_in);
+
+/*
+ * Selective state space scan: D channels with N states each,
+ *     dt = softplus(delta_k + delta_bias)   (MEBPTT_SCAN_SOFTPLUS; else dt = delta_k + delta_bias)
+ *     s_k[n] = exp(dt A[n]) s_{k-1}[n] + dt u_k B_k[n]
+ *     v_k = sum_n C_k[n] s_k[n] + skip u_k,      y_k = v_k silu(z_k), or v_k without a gate.
+ * Channels come in `groups` of D / groups that share B and C.
+ *   u, delta, z, y [t][B][D] and Bm, Cm [t][B][groups * N], operand type (z nullable: no gate);
+ *   A [D][N], skip [D], delta_bias [D] float32 (the last two nullable: zeros);
+ *   states and their gradients [B][D][N] float32; dA, dskip, ddelta_bias float32.
+ * A is expected to be negative and dt positive, so that states fade; others are computed as written.
+ * 1 <= N <= 64.
+ *
+ * kept (nullable for the forward call: nothing will be differentiated): a buffer of
+ * mebptt_scan_kept_bytes() which the caller holds between the two calls; it takes the states before
+ * steps 0, spacing, 2 spacing, ... in float32.  spacing is 8, 16 or 32: memory against time, since with
+ * more than 8 the backward pass recomputes states twice.
+ */
+enum { MEBPTT_SCAN_SOFTPLUS = 1 };
+typedef struct {
+  int32_t batch, channels, states, groups;
+  int32_t dtype;
+  int32_t flags;               /* MEBPTT_SCAN_SOFTPLUS or 0 */
+  int32_t spacing;
+  int32_t reserved;            /* 0 */
+  int64_t t;
+  int64_t u_step, u_row;       /* of u and du; the others likewise */
+  int64_t delta_step, delta_row;
+  int64_t z_step, z_row;
+  int64_t b_step, b_row;
+  int64_t c_step, c_row;
+  int64_t y_step, y_row;       /* of y and dy */
+} mebptt_scan_desc;
+
+size_t mebptt_scan_kept_bytes(const mebptt_scan_desc *desc);
+/* Device workspace of mebptt_scan_forward (backward = 0) or of both calls (1); 0: none, or a bad descriptor. */
+size_t mebptt_scan_workspace_bytes(const mebptt_scan_desc *desc, int backward);
+int mebptt_scan_forward(const mebptt_scan_desc *desc, const void *u, const void *delta, const float *A,
+                        const void *Bm, const void *Cm, const float *skip, const void *z,
+                        const float *delta_bias, const float *s_in, const int32_t *lengths,
+                        void *workspace, size_t workspace_bytes, void *stream,
+                        void *y, float *s_out, void *kept);
+/* Inputs, lengths and kept as in (and from) the forward call.  dskip, ddelta_bias, ds_in may be NULL; dz is wanted
+ * if and only if there is a gate. */
+int mebptt_scan_backward(const mebptt_scan_desc *desc, const void *u, const void *delta, const float *A,
+                         const void *Bm, const void *Cm, const float *skip, const void *z,
+                         const float *delta_bias, const int32_t *lengths, const void *kept,
+                         const void *dy, const float *ds_out,
+                         void *workspace, size_t workspace_bytes, void *stream,
+                         void *du, void *ddelta, float *dA, void *dB, void *dC, float *dskip, void *dz,
+                         float *ddelta_bias, float *ds_in);
+
+/*
+ * Distillation from a teacher's top logits.  Row r of the student's logits is compared with the
+ * `entries` tokens that the teacher found most likely:
+ *     p = softmax(logits_r / T) over the vocabulary,   q = softmax(values_r / T) over the row's entries,
+ *     row_loss_r = w_r T^2 sum_j q_j (log q_j - log p[indices_rj]),     loss = scale sum_r row_loss_r,
+ *     dlogits_r = dloss scale w_r T (p - q at the listed tokens).
+ *   logits, dlogits [rows][vocabulary] operand type, rows logits_row and dlogits_row elements apart
+ *   (0: vocabulary); indices int32, values float32 [rows][entries]; weights [rows] float32 (nullable: ones);
+ *   dloss: one float32 on the device (nullable: 1); loss: one float32 (nullable).
+ * An entry whose index is outside 0 .. vocabulary - 1 or whose value is -infinity is not there (padding);
+ * a token listed more than once counts with the sum of its q.  A row without entries, or of weight 0, has loss 0 and a gradient of
+ * zeros, whatever its logits are.  1 <= entries <= 1024.  dlogits may be logits itself (with the same
+ * row stride).
+ *
+ *   mebptt_distill_loss       losses, and row_stats [rows][2] for the gradient: a row's largest logit and
+ *                             sum_v exp((logit_v - largest) / T) (0, 1 for rows that count nothing)
+ *   mebptt_distill_grad       the gradient, from row_stats
+ *   mebptt_distill_loss_grad  both, reading the logits once
+ */
+typedef struct {
+  int64_t rows;
+  int32_t vocabulary, entries;
+  int32_t dtype;
+  int32_t reserved;            /* 0 */
+  float temperature, scale;    /* temperature > 0 */
+  int64_t logits_row, dlogits_row;
+} mebptt_distill_desc;
+
+int mebptt_distill_loss(const mebptt_distill_desc *desc, const void *logits, const int32_t *indices,
+                        const float *values, const float *weights, void *stream,
+                        float *loss, float *row_loss, float *row_stats);
+int mebptt_distill_grad(const mebptt_distill_desc *desc, const void *logits, const int32_t *indices,
+                        const float *values, const float *weights, const float *row_stats,
+                        const float *dloss, void *stream, void *dlogits);
+int mebptt_distill_loss_grad(const mebptt_distill_desc *desc, const void *logits, const int32_t *indices,
+                             const float *values, const float *weights, const float *dloss, void *stream,
+                             float *loss, float *row_loss, void *dlogits);
+
 /*
  * Testing aid for the bounded waits of the kernels whose CTAs wait for one another (no counterpart in
  * the paper).  Every wait of those kernels on a step counter or a barrier gives up after a bounded number of

@@ -10,6 +10,9 @@ written from the paper's equations:
                     the DP tables; they pin ``policy``.
 * ``lstm_bptt``  -- standard full-memory BPTT (Section 2.1) of a stacked LSTM with a linear
                     readout and a per-step MSE loss, in float64.
+* ``sequence_ops`` -- the short causal convolution, the selective scan and the distillation
+                    loss, forward and backward, in numbers (``bounded``) that carry a bound of
+                    what float32 may make of them.
 
 Only the test-suite, the smoke check and the benchmark's CPU-baseline leg may import this
 package.  It shares no code with the CUDA library and never receives values from it.

@@ -49,6 +49,25 @@ class mebptt_lstm_desc(C.Structure):
                 ("want_dx", C.c_int32), ("flags", C.c_int32), ("t", C.c_int64)]
 
 
+class mebptt_conv_desc(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("channels", C.c_int32), ("width", C.c_int32), ("dtype", C.c_int32),
+                ("flags", C.c_int32), ("reserved", C.c_int32), ("t", C.c_int64), ("x_step", C.c_int64),
+                ("x_row", C.c_int64), ("y_step", C.c_int64), ("y_row", C.c_int64)]
+
+
+class mebptt_scan_desc(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("channels", C.c_int32), ("states", C.c_int32), ("groups", C.c_int32),
+                ("dtype", C.c_int32), ("flags", C.c_int32), ("spacing", C.c_int32), ("reserved", C.c_int32),
+                ("t", C.c_int64)] + [(f"{a}_{s}", C.c_int64) for a in ("u", "delta", "z", "b", "c", "y")
+                                     for s in ("step", "row")]
+
+
+class mebptt_distill_desc(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("vocabulary", C.c_int32), ("entries", C.c_int32), ("dtype", C.c_int32),
+                ("reserved", C.c_int32), ("temperature", C.c_float), ("scale", C.c_float),
+                ("logits_row", C.c_int64), ("dlogits_row", C.c_int64)]
+
+
 _vp, _i64, _i32, _sz = C.c_void_p, C.c_int64, C.c_int, C.c_size_t
 _descp = C.POINTER(mebptt_lstm_desc)
 _STEP_ARGS = [_descp, _vp] + [_vp] * 8 + [_vp, _sz, _vp] + [_vp] * 7
@@ -98,6 +117,16 @@ _SIGS = {
     "mebptt_test_launches": (_i64, []),
     "mebptt_slot_copy": (_i32, [_vp, _vp, _sz, _vp]),
     "mebptt_gemm_bf16": (_i32, [_vp, _i64, _i32, _vp, _i64, _i32, _vp, _i64, _i32, _vp, _i64, _i64, _i64, _vp, _vp]),
+    "mebptt_conv_forward": (_i32, [_vp] * 9),
+    "mebptt_conv_workspace_bytes": (_sz, [_vp]),
+    "mebptt_conv_backward": (_i32, [_vp] * 9 + [_sz] + [_vp] * 5),
+    "mebptt_scan_kept_bytes": (_sz, [_vp]),
+    "mebptt_scan_workspace_bytes": (_sz, [_vp, _i32]),
+    "mebptt_scan_forward": (_i32, [_vp] * 12 + [_sz] + [_vp] * 4),
+    "mebptt_scan_backward": (_i32, [_vp] * 14 + [_sz] + [_vp] * 10),
+    "mebptt_distill_loss": (_i32, [_vp] * 9),
+    "mebptt_distill_grad": (_i32, [_vp] * 9),
+    "mebptt_distill_loss_grad": (_i32, [_vp] * 10),
     "mebptt_strerror": (C.c_char_p, [_i32]),
 }
 for _name, (_res, _args) in _SIGS.items():
@@ -381,3 +410,124 @@ def mebptt_gemm_bf16(A, lda, a_major, Bm, ldb, b_major, Cm, ldc, accumulate, bia
 
 def mebptt_slot_copy(dst, src, nbytes: int, stream=None):
     _check(lib.mebptt_slot_copy(_ptr(dst), _ptr(src), nbytes, stream), "mebptt_slot_copy")
+
+
+# ---- operators over sequences ----------------------------------------------------------------------------------------
+# Arrays over time are torch tensors [t, batch, width], of any strides along t and batch: a descriptor holds those strides
+# (x.stride(0), x.stride(1)), so one descriptor serves all arrays that lie alike.
+
+MEBPTT_CONV_SILU = 1
+MEBPTT_SCAN_SOFTPLUS = 1
+
+
+def _dtype(d) -> int:
+    return DTYPES[d] if isinstance(d, str) else d
+
+
+def make_conv_desc(batch, channels, width, t, dtype, silu=True, x_strides=(0, 0), y_strides=(0, 0)) -> mebptt_conv_desc:
+    """Strides are (step, row) in elements; (0, 0) stands for a dense array, time-major."""
+    return mebptt_conv_desc(batch, channels, width, _dtype(dtype), MEBPTT_CONV_SILU if silu else 0, 0, t, *x_strides, *y_strides)
+
+
+def make_scan_desc(batch, channels, states, groups, t, dtype, softplus=True, spacing=8, u_strides=(0, 0), delta_strides=(0, 0),
+                   z_strides=(0, 0), B_strides=(0, 0), C_strides=(0, 0), y_strides=(0, 0)) -> mebptt_scan_desc:
+    """Strides are (step, row) in elements; (0, 0) stands for a dense array, time-major."""
+    return mebptt_scan_desc(batch, channels, states, groups, _dtype(dtype), MEBPTT_SCAN_SOFTPLUS if softplus else 0, spacing, 0, t,
+                            *u_strides, *delta_strides, *z_strides, *B_strides, *C_strides, *y_strides)
+
+
+def make_distill_desc(rows, vocabulary, entries, dtype, temperature=1.0, scale=1.0, logits_row=0, dlogits_row=0) -> mebptt_distill_desc:
+    return mebptt_distill_desc(rows, vocabulary, entries, _dtype(dtype), 0, temperature, scale, logits_row, dlogits_row)
+
+
+_OPERANDS = {MEBPTT_BF16: ("torch.bfloat16", 2), MEBPTT_FP32: ("torch.float32", 4), MEBPTT_TF32: ("torch.float32", 4)}
+
+
+def _typed(name, dtype, operands, floats, ints=()):
+    """Raises where a tensor's type is not what the call takes it for (a wrong one would be read past its end)."""
+    want = _OPERANDS.get(dtype)
+    for group, kind in ((operands, want and want[0]), (floats, "torch.float32"), (ints, "torch.int32")):
+        for x in group:
+            if x is not None and not (x.is_cuda and _NAMES.get(x.dtype) == kind):
+                raise MebpttError(MEBPTT_ERR_ARG, f"{name}: a {x.dtype} tensor on {x.device} where a CUDA tensor of {kind} belongs")
+
+
+class _Names(dict):
+    def __missing__(self, dtype):
+        self[dtype] = str(dtype)
+        return self[dtype]
+
+    def get(self, dtype):
+        return self[dtype]
+
+
+_NAMES = _Names()
+
+
+def mebptt_conv_forward(desc, x, w, bias, s_in, lengths, stream, y, s_out):
+    _typed("mebptt_conv_forward", desc.dtype, (x, w, s_in, y, s_out), (bias,), (lengths,))
+    st = lib.mebptt_conv_forward(C.addressof(desc), _ptr(x), _ptr(w), _ptr(bias), _ptr(s_in), _ptr(lengths), stream, _ptr(y), _ptr(s_out))
+    _check(st, "mebptt_conv_forward")
+
+
+def mebptt_conv_workspace_bytes(desc) -> int:
+    return lib.mebptt_conv_workspace_bytes(C.addressof(desc))
+
+
+def mebptt_conv_backward(desc, x, w, bias, s_in, lengths, dy, ds_out, workspace, stream, dx, dw, dbias, ds_in):
+    _typed("mebptt_conv_backward", desc.dtype, (x, w, s_in, dy, ds_out, dx, ds_in), (bias, dw, dbias), (lengths,))
+    st = lib.mebptt_conv_backward(C.addressof(desc), _ptr(x), _ptr(w), _ptr(bias), _ptr(s_in), _ptr(lengths), _ptr(dy), _ptr(ds_out),
+                                  _ptr(workspace), _nbytes(workspace), stream, _ptr(dx), _ptr(dw), _ptr(dbias), _ptr(ds_in))
+    _check(st, "mebptt_conv_backward")
+
+
+def mebptt_scan_kept_bytes(desc) -> int:
+    return lib.mebptt_scan_kept_bytes(C.addressof(desc))
+
+
+def mebptt_scan_workspace_bytes(desc, backward=False) -> int:
+    return lib.mebptt_scan_workspace_bytes(C.addressof(desc), int(backward))
+
+
+def mebptt_scan_forward(desc, u, delta, A, Bm, Cm, skip, z, delta_bias, s_in, lengths, workspace, stream, y, s_out, kept=None):
+    _typed("mebptt_scan_forward", desc.dtype, (u, delta, Bm, Cm, z, y), (A, skip, delta_bias, s_in, s_out), (lengths,))
+    if kept is not None and _nbytes(kept) < mebptt_scan_kept_bytes(desc):
+        raise MebpttError(MEBPTT_ERR_WORKSPACE, "mebptt_scan_forward: kept")
+    st = lib.mebptt_scan_forward(C.addressof(desc), _ptr(u), _ptr(delta), _ptr(A), _ptr(Bm), _ptr(Cm), _ptr(skip), _ptr(z),
+                                 _ptr(delta_bias), _ptr(s_in), _ptr(lengths), _ptr(workspace),
+                                 0 if workspace is None else _nbytes(workspace), stream, _ptr(y), _ptr(s_out), _ptr(kept))
+    _check(st, "mebptt_scan_forward")
+
+
+def mebptt_scan_backward(desc, u, delta, A, Bm, Cm, skip, z, delta_bias, lengths, kept, dy, ds_out, workspace, stream, du, ddelta,
+                         dA, dB, dC, dskip, dz, ddelta_bias, ds_in):
+    _typed("mebptt_scan_backward", desc.dtype, (u, delta, Bm, Cm, z, dy, du, ddelta, dB, dC, dz),
+           (A, skip, delta_bias, ds_out, dA, dskip, ddelta_bias, ds_in), (lengths,))
+    if kept is not None and _nbytes(kept) < mebptt_scan_kept_bytes(desc):
+        raise MebpttError(MEBPTT_ERR_WORKSPACE, "mebptt_scan_backward: kept")
+    st = lib.mebptt_scan_backward(C.addressof(desc), _ptr(u), _ptr(delta), _ptr(A), _ptr(Bm), _ptr(Cm), _ptr(skip), _ptr(z),
+                                  _ptr(delta_bias), _ptr(lengths), _ptr(kept), _ptr(dy), _ptr(ds_out), _ptr(workspace),
+                                  0 if workspace is None else _nbytes(workspace), stream, _ptr(du), _ptr(ddelta), _ptr(dA), _ptr(dB),
+                                  _ptr(dC), _ptr(dskip), _ptr(dz), _ptr(ddelta_bias), _ptr(ds_in))
+    _check(st, "mebptt_scan_backward")
+
+
+def mebptt_distill_loss(desc, logits, indices, values, weights, stream, loss, row_loss, row_stats):
+    _typed("mebptt_distill_loss", desc.dtype, (logits,), (values, weights, loss, row_loss, row_stats), (indices,))
+    st = lib.mebptt_distill_loss(C.addressof(desc), _ptr(logits), _ptr(indices), _ptr(values), _ptr(weights), stream, _ptr(loss),
+                                 _ptr(row_loss), _ptr(row_stats))
+    _check(st, "mebptt_distill_loss")
+
+
+def mebptt_distill_grad(desc, logits, indices, values, weights, row_stats, dloss, stream, dlogits):
+    _typed("mebptt_distill_grad", desc.dtype, (logits, dlogits), (values, weights, row_stats, dloss), (indices,))
+    st = lib.mebptt_distill_grad(C.addressof(desc), _ptr(logits), _ptr(indices), _ptr(values), _ptr(weights), _ptr(row_stats),
+                                 _ptr(dloss), stream, _ptr(dlogits))
+    _check(st, "mebptt_distill_grad")
+
+
+def mebptt_distill_loss_grad(desc, logits, indices, values, weights, dloss, stream, loss, row_loss, dlogits):
+    _typed("mebptt_distill_loss_grad", desc.dtype, (logits, dlogits), (values, weights, dloss, loss, row_loss), (indices,))
+    st = lib.mebptt_distill_loss_grad(C.addressof(desc), _ptr(logits), _ptr(indices), _ptr(values), _ptr(weights), _ptr(dloss), stream,
+                                      _ptr(loss), _ptr(row_loss), _ptr(dlogits))
+    _check(st, "mebptt_distill_loss_grad")

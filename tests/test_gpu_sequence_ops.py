@@ -1,0 +1,354 @@
+"""GPU: convolution, scan and distillation loss against the float64 oracle, element by element within the bounds it derives."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import sequence_ops as O
+from paper_1606_03401_b200 import binding as B
+from tests.seq_util import Laid, assert_within, device, numpy, rounded
+
+pytestmark = pytest.mark.gpu
+
+
+def _stream():
+    return torch.cuda.current_stream().cuda_stream
+
+
+def _lengths(r, n, t, ragged):
+    if not ragged:
+        return None
+    v = r.integers(0, t + 1, n)
+    v[0] = t
+    if n > 1:
+        v[1] = 0
+    if n > 2:
+        v[2] = 1
+    return v
+
+
+def _hide(a, lengths):
+    """NaN and infinities where a row has no steps."""
+    if lengths is not None:
+        for b, n in enumerate(lengths):
+            a[n:, b] = np.nan
+            a[n::2, b] = np.inf
+    return a
+
+
+class Conv:
+    def __init__(self, dtype, N, t, D, W, layout="time", silu=True, state=True, ragged=True, bias=True, seed=0):
+        r = np.random.default_rng(seed)
+        self.dtype, self.silu = dtype, silu
+        self.lengths = _lengths(r, N, t, ragged)
+        self.x, self.dy = (_hide(rounded(r.standard_normal((t, N, D)), dtype), self.lengths) for _ in range(2))
+        self.w, self.bias = rounded(r.standard_normal((D, W)), dtype), rounded(r.standard_normal(D), "fp32") if bias else None
+        self.s_in, self.ds_out = (rounded(r.standard_normal((N, W - 1, D)), dtype) if state else None for _ in range(2))
+        self.X, self.DY = Laid(self.x.shape, dtype, layout, self.x), Laid(self.x.shape, dtype, layout, self.dy)
+        self.Y, self.DX = Laid(self.x.shape, dtype, layout), Laid(self.x.shape, dtype, layout)
+        self.desc = B.make_conv_desc(N, D, W, t, dtype, silu, self.X.strides, self.Y.strides)
+        self.dev = dict(w=device(self.w, dtype), bias=device(self.bias), s_in=device(self.s_in, dtype), ds_out=device(self.ds_out, dtype),
+                        lengths=None if self.lengths is None else torch.tensor(self.lengths, dtype=torch.int32, device="cuda"))
+        st = lambda: torch.full((N, W - 1, D), 7.0, device="cuda").to(self.X.x.dtype) if state else None  # noqa: E731
+        self.s_out, self.ds_in = st(), st()
+        self.dw, self.dbias = torch.full((D, W), 7.0, device="cuda"), torch.full((D,), 7.0, device="cuda") if bias else None
+        self.workspace = torch.full((B.mebptt_conv_workspace_bytes(self.desc),), 255, dtype=torch.uint8, device="cuda")
+
+    def forward(self):
+        d = self.dev
+        B.mebptt_conv_forward(self.desc, self.X.x, d["w"], d["bias"], d["s_in"], d["lengths"], _stream(), self.Y.x, self.s_out)
+
+    def backward(self):
+        d = self.dev
+        B.mebptt_conv_backward(self.desc, self.X.x, d["w"], d["bias"], d["s_in"], d["lengths"], self.DY.x, d["ds_out"], self.workspace,
+                               _stream(), self.DX.x, self.dw, self.dbias, self.ds_in)
+
+    def outputs(self):
+        return [v for v in (self.Y.x, self.s_out, self.DX.x, self.dw, self.dbias, self.ds_in) if v is not None]
+
+    def check(self):
+        z = lambda a: np.nan_to_num(a, nan=0.0, posinf=0.0) if self.lengths is not None else a  # noqa: E731  (not read)
+        ref = O.conv(z(self.x), self.w, self.bias, self.s_in, self.lengths, self.silu, z(self.dy), self.ds_out)
+        got = {"y": (self.Y.numpy(), self.dtype), "dx": (self.DX.numpy(), self.dtype), "dw": (numpy(self.dw), "fp32")}
+        if self.bias is not None:
+            got["dbias"] = (numpy(self.dbias), "fp32")
+        if self.s_in is not None:
+            got.update(s_out=(numpy(self.s_out), self.dtype), ds_in=(numpy(self.ds_in), self.dtype))
+        for k, (v, dtype) in got.items():
+            assert_within(k, v, ref[k], ref["bound"][k], dtype)
+        assert all(a.untouched() for a in (self.X, self.Y, self.DX, self.DY))
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("N,t,D,W,layout,kw", [
+    (1, 1, 1, 4, "time", {}),
+    (1, 2, 8, 8, "time", {}),                                   # fewer steps than the window
+    (4, 9, 40, 4, "time", {}),
+    (3, 33, 300, 3, "batch", {}),
+    (3, 20, 37, 5, "odd", {}),
+    (2, 50, 64, 4, "sliced", dict(silu=False)),
+    (5, 17, 24, 2, "sliced", dict(state=False)),
+    (3, 12, 520, 6, "time", dict(ragged=False, bias=False)),
+    (2, 31, 16, 7, "batch", dict(ragged=False, state=False)),
+    (9, 5, 264, 1, "time", {}),
+])
+def test_conv_matches_the_oracle(dtype, N, t, D, W, layout, kw):
+    p = Conv(dtype, N, t, D, W, layout, **kw)
+    p.forward()
+    p.backward()
+    p.check()
+
+
+class Scan:
+    def __init__(self, dtype, N, t, D, S, G=1, spacing=8, layout="time", gate=True, state=True, ragged=True, soft=True, extras=True, seed=0):
+        r = np.random.default_rng(seed)
+        self.dtype, self.soft, self.G = dtype, soft, G
+        self.lengths = L = _lengths(r, N, t, ragged)
+        draw = lambda *s: _hide(rounded(r.standard_normal(s), dtype), L)  # noqa: E731
+        self.in_ = {"u": draw(t, N, D), "delta": draw(t, N, D) - 0.0, "Bm": draw(t, N, G * S), "Cm": draw(t, N, G * S),
+                    "z": draw(t, N, D) if gate else None, "dy": draw(t, N, D)}
+        if not soft:
+            self.in_["delta"] = rounded(np.abs(self.in_["delta"]) * 0.25, dtype)
+        self.A = rounded(-np.exp(r.standard_normal((D, S))), "fp32")
+        self.skip, self.bias = (rounded(r.standard_normal(D), "fp32") if extras else None for _ in range(2))
+        if extras:
+            self.bias = rounded(np.abs(self.bias) - (2 if soft else 0), "fp32")
+        self.s_in, self.ds_out = (rounded(r.standard_normal((N, D, S)), "fp32") if state else None for _ in range(2))
+        lay = lambda a: None if a is None else Laid(a.shape, dtype, layout, a)  # noqa: E731
+        self.L = {k: lay(v) for k, v in self.in_.items()}
+        out = lambda k: None if self.in_[k] is None else Laid(self.in_[k].shape, dtype, layout)  # noqa: E731
+        self.Lo = {"y": out("u"), "du": out("u"), "ddelta": out("delta"), "dz": out("z"), "dB": out("Bm"), "dC": out("Cm")}
+        at = {n + "_strides": self.L[k].strides for n, k in (("u", "u"), ("delta", "delta"), ("z", "z"), ("B", "Bm"), ("C", "Cm"), ("y", "dy")) if self.L[k]}
+        self.desc = B.make_scan_desc(N, D, S, G, t, dtype, soft, spacing, **at)
+        self.dev = dict(A=device(self.A), skip=device(self.skip), bias=device(self.bias), s_in=device(self.s_in), ds_out=device(self.ds_out),
+                        lengths=None if L is None else torch.tensor(L, dtype=torch.int32, device="cuda"))
+        new = lambda *s: torch.full(s, 7.0, device="cuda")  # noqa: E731
+        self.s_out, self.ds_in, self.dA = new(N, D, S), new(N, D, S) if state else None, new(D, S)
+        self.dskip, self.dbias = (new(D) if extras else None for _ in range(2))
+        self.workspace = torch.full((B.mebptt_scan_workspace_bytes(self.desc, True),), 255, dtype=torch.uint8, device="cuda")
+        self.kept = torch.full((B.mebptt_scan_kept_bytes(self.desc),), 255, dtype=torch.uint8, device="cuda")
+
+    def _x(self, *names):
+        return [None if self.L[k] is None else self.L[k].x for k in names]
+
+    def forward(self, keep=True):
+        d = self.dev
+        u, delta, Bm, Cm, z = self._x("u", "delta", "Bm", "Cm", "z")
+        B.mebptt_scan_forward(self.desc, u, delta, d["A"], Bm, Cm, d["skip"], z, d["bias"], d["s_in"], d["lengths"], self.workspace, _stream(),
+                              self.Lo["y"].x, self.s_out, self.kept if keep else None)
+
+    def backward(self):
+        d = self.dev
+        u, delta, Bm, Cm, z, dy = self._x("u", "delta", "Bm", "Cm", "z", "dy")
+        o = {k: None if v is None else v.x for k, v in self.Lo.items()}
+        B.mebptt_scan_backward(self.desc, u, delta, d["A"], Bm, Cm, d["skip"], z, d["bias"], d["lengths"], self.kept, dy, d["ds_out"],
+                               self.workspace, _stream(), o["du"], o["ddelta"], self.dA, o["dB"], o["dC"], self.dskip, o["dz"], self.dbias,
+                               self.ds_in)
+
+    def outputs(self):
+        return [v.x for v in self.Lo.values() if v is not None] + [v for v in (self.s_out, self.ds_in, self.dA, self.dskip, self.dbias) if v is not None]
+
+    def check(self):
+        z = {k: None if v is None else np.nan_to_num(v, nan=0.0, posinf=0.0) for k, v in self.in_.items()}
+        ref = O.scan(z["u"], z["delta"], self.A, z["Bm"], z["Cm"], self.skip, z["z"], self.bias, self.s_in, self.lengths, self.soft,
+                     z["dy"], self.ds_out, self.G)
+        for k, v in self.Lo.items():
+            if v is not None:
+                assert_within(k, v.numpy(), ref[k], ref["bound"][k], self.dtype)
+                assert v.untouched(), k
+        for k, v in (("s_out", self.s_out), ("ds_in", self.ds_in), ("dA", self.dA), ("dskip", self.dskip), ("ddelta_bias", self.dbias)):
+            if v is not None:
+                assert_within(k, numpy(v), ref[k], ref["bound"][k], "fp32")
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("N,t,D,S,kw", [
+    (1, 1, 1, 1, dict(ragged=False)),
+    (3, 1, 40, 16, {}),
+    (3, 2, 5, 3, {}),
+    (2, 33, 64, 16, dict(spacing=16)),
+    (3, 32, 72, 16, dict(layout="batch")),
+    (3, 70, 37, 10, dict(layout="odd", spacing=32)),
+    (2, 41, 24, 16, dict(layout="sliced", G=3)),
+    (2, 40, 300, 4, dict(state=False)),
+    (2, 37, 150, 7, dict(spacing=32, gate=False)),
+    (2, 50, 48, 20, dict(soft=False)),
+    (2, 35, 20, 64, dict(G=2)),
+    (2, 34, 17, 33, dict(extras=False, spacing=16)),
+    (1, 300, 16, 16, dict(ragged=False)),                       # segments
+    (2, 260, 24, 8, dict(spacing=32, layout="batch")),
+    (3, 200, 12, 32, dict(spacing=16, G=2)),
+    (3, 200, 9, 4, dict(state=False, gate=False)),
+])
+def test_scan_matches_the_oracle(dtype, N, t, D, S, kw):
+    p = Scan(dtype, N, t, D, S, **kw)
+    p.forward()
+    p.backward()
+    p.check()
+
+
+def test_scan_without_kept_states_and_with_a_state_in_place():
+    p = Scan("bf16", 3, 300, 24, 16, ragged=True)
+    p.forward()
+    y, s = p.Lo["y"].x.clone(), p.s_out.clone()
+    p.Lo["y"].x.zero_()
+    p.s_out = p.dev["s_in"]                                     # over the state it begins with, in segments
+    p.forward(keep=False)
+    assert torch.equal(p.Lo["y"].x, y) and torch.equal(p.s_out, s)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_token_by_token_is_the_prompt(dtype):
+    """A prompt in one call, and the same steps one at a time with the states in place."""
+    t, N, D, S, W = 12, 3, 40, 16, 4
+    c, s = Conv(dtype, N, t, D, W, ragged=False), Scan(dtype, N, t, D, S, ragged=False)
+    c.forward()
+    s.forward()
+    cd, sd = B.make_conv_desc(N, D, W, 1, dtype), B.make_scan_desc(N, D, S, 1, 1, dtype)
+    cs, ss = c.dev["s_in"].clone(), s.dev["s_in"].clone()
+    for k in range(t):
+        y, v = torch.empty(N, D, dtype=c.X.x.dtype, device="cuda"), torch.empty(N, D, dtype=c.X.x.dtype, device="cuda")
+        B.mebptt_conv_forward(cd, c.X.x[k], c.dev["w"], c.dev["bias"], cs, None, _stream(), y, cs)
+        assert torch.equal(y, c.Y.x[k])
+        u, delta, Bm, Cm, z = (x[k] for x in s._x("u", "delta", "Bm", "Cm", "z"))
+        B.mebptt_scan_forward(sd, u, delta, s.dev["A"], Bm, Cm, s.dev["skip"], z, s.dev["bias"], ss, None, None, _stream(), v, ss)
+        # the same operations in the same order but for the sum over states
+        assert torch.allclose(v.float(), s.Lo["y"].x[k].float(), rtol=2 ** -7 if dtype == "bf16" else 1e-5, atol=1e-5)
+    assert torch.equal(cs, c.s_out) and torch.allclose(ss, s.s_out, rtol=1e-6, atol=1e-7)
+
+
+class Distill:
+    def __init__(self, dtype, R, V, K, T=1.0, weights=True, pad=0, phase=0, seed=0, scale=None):
+        r = np.random.default_rng(seed)
+        self.dtype, self.T, self.scale = dtype, T, float(np.float32(1.0 / R if scale is None else scale))
+        self.x = rounded(3 * r.standard_normal((R, V)), dtype)
+        self.i = np.stack([r.permutation(V)[:K] if K <= V else r.integers(0, V, K) for _ in range(R)])
+        self.v = rounded(2 * r.standard_normal((R, K)), "fp32")
+        self.w = rounded(r.random(R) + 0.1, "fp32") if weights else None
+        self.row = V + pad
+        self.memory = torch.full((phase + R * self.row,), 977.0, device="cuda").to(device(self.x[:1], dtype).dtype)
+        self.X = self.memory.as_strided((R, V), (self.row, 1), phase)
+        self.dmemory = self.memory.clone()
+        self.DX = self.dmemory.as_strided((R, V), (self.row, 1), phase)
+        self.desc = B.make_distill_desc(R, V, K, dtype, T, self.scale, self.row, self.row)
+        self.loss, self.row_loss, self.stats = (torch.full((n,), 7.0, device="cuda") for n in (1, R, 2 * R))
+        self.dloss = torch.full((1,), 0.5, device="cuda")
+
+    def upload(self):
+        self.X.copy_(torch.from_numpy(self.x))
+        self.dev = (torch.tensor(self.i, dtype=torch.int32, device="cuda"), device(self.v), device(self.w))
+        return self
+
+    def both(self):
+        B.mebptt_distill_loss_grad(self.desc, self.X, *self.dev, self.dloss, _stream(), self.loss, self.row_loss, self.DX)
+
+    def apart(self):
+        B.mebptt_distill_loss(self.desc, self.X, *self.dev, _stream(), self.loss, self.row_loss, self.stats)
+        B.mebptt_distill_grad(self.desc, self.X, *self.dev, self.stats, self.dloss, _stream(), self.DX)
+
+    def check(self):
+        ref = O.distill(self.x, self.i, self.v, self.w, float(np.float32(self.T)), self.scale, 0.5)
+        assert_within("loss", numpy(self.loss)[0], ref["loss"], ref["bound"]["loss"], "fp32")
+        assert_within("row_loss", numpy(self.row_loss), ref["row_loss"], ref["bound"]["row_loss"], "fp32")
+        assert_within("dlogits", numpy(self.DX), ref["dlogits"], ref["bound"]["dlogits"], self.dtype)
+        R, V = self.x.shape
+        if self.row > V:
+            assert bool((self.dmemory.as_strided((R - 1, self.row - V), (self.row, 1), self.DX.storage_offset() + V) == 977.0).all()) if R > 1 else True
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("R,V,K,kw", [
+    (1, 1, 1, {}),
+    (3, 7, 7, dict(T=0.5)),
+    (5, 33, 4, dict(pad=3)),
+    (40, 1024, 16, dict(T=2.0)),
+    (3, 1000, 100, dict(phase=1)),
+    (4, 5003, 33, dict(weights=False, phase=3, pad=1)),
+    (2, 40000, 64, dict(T=1.5)),
+    (400, 2048, 8, dict(T=4.0)),
+    (2, 140001, 20, {}),                                        # longer than the registers of a cluster
+    (2, 300000, 20, dict(T=3.0)),
+])
+def test_distill_matches_the_oracle(dtype, R, V, K, kw):
+    p = Distill(dtype, R, V, K, **kw).upload()
+    p.both()
+    p.check()
+    p.DX.fill_(7.0)
+    p.apart()
+    p.check()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("V,K", [(50, 12), (20000, 700)])
+def test_distill_entries_that_repeat_or_are_not_there(dtype, V, K):
+    p = Distill(dtype, 8, V, K)
+    p.i[0] = 5                                                  # one token, K times
+    p.i[1] = np.random.default_rng(1).integers(0, 4, K)         # four tokens
+    p.i[2, 3:] = -1
+    p.i[3] = -1                                                 # no entry
+    p.i[4, ::2] = V                                             # past the vocabulary
+    p.v[5, 1:] = -np.inf
+    p.v[6] = -np.inf                                            # no entry either
+    p.w[7] = 0
+    lowest = float(torch.finfo(p.X.dtype).min)
+    p.upload()
+    p.both()
+    p.check()
+    p.DX.fill_(7.0)
+    p.apart()
+    p.check()
+    # masked tokens: logits of -inf and of the type's lowest value; rows that count nothing may hold anything
+    p.x[:, 20:40] = -np.inf
+    p.x[:, 40:45] = lowest
+    for r in range(8):
+        p.i[r][(p.i[r] >= 20) & (p.i[r] < 45)] = -1
+    p.upload()
+    p.X[3], p.X[6], p.X[7] = float("nan"), float("inf"), float("nan")
+    p.both()
+    p.check()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_distill_row_of_lowest_values_is_uniform_and_in_place(dtype):
+    p = Distill(dtype, 3, 3000, 5)
+    p.x[1] = float(torch.finfo(p.X.dtype).min)
+    p.upload()
+    p.DX, p.dmemory = p.X, p.memory                             # the gradient over the logits
+    p.both()
+    p.check()
+    p.upload()
+    B.mebptt_distill_loss(p.desc, p.X, *p.dev, _stream(), p.loss, p.row_loss, p.stats)
+    B.mebptt_distill_grad(p.desc, p.X, *p.dev, p.stats, p.dloss, _stream(), p.X)
+    p.check()
+
+
+@pytest.mark.parametrize("make", [lambda: Conv("bf16", 4, 60, 72, 4), lambda: Scan("bf16", 2, 300, 40, 16), lambda: Scan("fp32", 2, 70, 40, 16, spacing=32),
+                                  lambda: Distill("bf16", 9, 5001, 12).upload()], ids=["conv", "scan", "scan_lean", "distill"])
+def test_captured_replayed_on_another_stream_and_bit_identical(make):
+    p = make()
+
+    def call():
+        if isinstance(p, Distill):
+            p.both()
+        else:
+            p.forward()
+            p.backward()
+
+    def outputs():
+        return [p.loss, p.row_loss, p.DX] if isinstance(p, Distill) else p.outputs()
+
+    call()
+    torch.cuda.synchronize()
+    want = [v.clone() for v in outputs()]
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a.nan_to_num(), b.nan_to_num()) for a, b in zip(outputs(), want))
+    with torch.cuda.graph(graph):
+        call()
+    for v in outputs():
+        v.fill_(3.0)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(outputs(), want))

@@ -1,0 +1,139 @@
+"""Refusals and sizes of the operators over sequences: nothing here reaches a device."""
+import ctypes as C
+
+import pytest
+
+from paper_1606_03401_b200 import binding as B
+
+P = 0x10000          # an address that is aligned to anything; never followed: every call below is refused first
+
+
+def _conv(back=False, desc=None, ws=P, nbytes=1 << 40, **kw):
+    d = desc or B.make_conv_desc(2, 24, 4, 10, "bf16")
+    for k, v in kw.items():
+        if hasattr(d, k):
+            setattr(d, k, v)
+    p = {k: kw.get(k, P) for k in ("x", "w", "bias", "s_in", "lengths", "y", "s_out", "dy", "ds_out", "dx", "dw", "dbias", "ds_in")}
+    if not back:
+        return B.lib.mebptt_conv_forward(C.addressof(d), p["x"], p["w"], p["bias"], p["s_in"], p["lengths"], None, p["y"], p["s_out"])
+    return B.lib.mebptt_conv_backward(C.addressof(d), p["x"], p["w"], p["bias"], p["s_in"], p["lengths"], p["dy"], p["ds_out"], ws, nbytes, None,
+                                      p["dx"], p["dw"], p["dbias"], p["ds_in"])
+
+
+def _scan(back=False, ws=P, nbytes=1 << 50, **kw):
+    d = B.make_scan_desc(2, 24, 16, 1, 10, "bf16")
+    for k, v in kw.items():
+        if k in dict(d._fields_):
+            setattr(d, k, v)
+    names = ("u", "delta", "A", "Bm", "Cm", "skip", "z", "bias", "s_in", "lengths", "y", "s_out", "kept", "dy", "ds_out", "du", "ddelta",
+             "dA", "dB", "dC", "dskip", "dz", "dbias", "ds_in")
+    p = {k: kw.get("p_" + k, P) for k in names}
+    if not back:
+        return B.lib.mebptt_scan_forward(C.addressof(d), *(p[k] for k in names[:10]), ws, nbytes, None, p["y"], p["s_out"], p["kept"])
+    return B.lib.mebptt_scan_backward(C.addressof(d), *(p[k] for k in names[:8]), p["lengths"], p["kept"], p["dy"], p["ds_out"], ws, nbytes, None,
+                                      *(p[k] for k in names[15:]))
+
+
+def _distill(which="both", **kw):
+    d = B.make_distill_desc(4, 100, 8, "bf16")
+    for k, v in kw.items():
+        if k in dict(d._fields_):
+            setattr(d, k, v)
+    p = {k: kw.get("p_" + k, P) for k in ("logits", "indices", "values", "weights", "dloss", "loss", "row_loss", "stats", "dlogits")}
+    a = (C.addressof(d), p["logits"], p["indices"], p["values"], p["weights"])
+    if which == "loss":
+        return B.lib.mebptt_distill_loss(*a, None, p["loss"], p["row_loss"], p["stats"])
+    if which == "grad":
+        return B.lib.mebptt_distill_grad(*a, p["stats"], p["dloss"], None, p["dlogits"])
+    return B.lib.mebptt_distill_loss_grad(*a, p["dloss"], None, p["loss"], p["row_loss"], p["dlogits"])
+
+
+@pytest.mark.parametrize("kw", [
+    dict(batch=0), dict(channels=0), dict(width=0), dict(width=9), dict(t=0), dict(t=(1 << 30) + 1), dict(dtype=3), dict(flags=2), dict(reserved=1),
+    dict(x=None), dict(w=None), dict(y=None), dict(x=P + 1), dict(w=P + 1), dict(s_in=P + 1), dict(bias=P + 2), dict(lengths=P + 2),
+    dict(x_step=-48, x_row=24), dict(x_step=23, x_row=24), dict(x_step=48, x_row=0), dict(y_step=0, y_row=24),
+    dict(x_step=24, x_row=100),                 # rows that begin inside one another
+    dict(y_step=47, y_row=24), dict(x_step=1 << 41, x_row=24),
+])
+def test_conv_forward_refuses(kw):
+    assert _conv(**kw) == B.MEBPTT_ERR_ARG
+
+
+def test_conv_backward_refuses():
+    for kw in (dict(dy=None), dict(dx=None), dict(dw=None), dict(dy=P + 1), dict(dw=P + 2), dict(dbias=P + 2), dict(ds_in=P + 1), dict(width=9)):
+        assert _conv(True, **kw) == B.MEBPTT_ERR_ARG, kw
+    need = B.mebptt_conv_workspace_bytes(B.make_conv_desc(2, 24, 4, 10, "bf16"))
+    assert need > 0
+    for ws, nbytes in ((None, need), (P + 128, need), (P, need - 1)):
+        assert _conv(True, ws=ws, nbytes=nbytes) == B.MEBPTT_ERR_WORKSPACE
+    assert B.mebptt_conv_workspace_bytes(B.make_conv_desc(2, 24, 9, 10, "bf16")) == 0
+
+
+@pytest.mark.parametrize("kw", [
+    dict(batch=0), dict(channels=0), dict(states=0), dict(states=65), dict(groups=0), dict(groups=5), dict(t=0), dict(dtype=-1), dict(flags=2),
+    dict(spacing=0), dict(spacing=12), dict(spacing=64), dict(reserved=1),
+    dict(u_step=10, u_row=24), dict(delta_step=24, delta_row=24), dict(z_step=-1, z_row=24), dict(b_step=31, b_row=16), dict(c_step=16, c_row=16),
+    dict(y_step=1, y_row=1), dict(p_u=None), dict(p_delta=None), dict(p_A=None), dict(p_Bm=None), dict(p_Cm=None), dict(p_u=P + 1), dict(p_A=P + 2),
+    dict(p_lengths=P + 1), dict(p_kept=P + 8),
+])
+@pytest.mark.parametrize("back", [False, True])
+def test_scan_refuses(back, kw):
+    assert _scan(back, **kw) == B.MEBPTT_ERR_ARG
+
+
+def test_scan_refuses_more():
+    assert _scan(p_y=None) == B.MEBPTT_ERR_ARG
+    for k in ("kept", "dy", "du", "ddelta", "dA", "dB", "dC", "dz", "z"):
+        assert _scan(True, **{"p_" + k: None}) == B.MEBPTT_ERR_ARG, k
+    for k in ("dB", "dA", "dskip", "dbias", "ds_out"):
+        assert _scan(True, **{"p_" + k: P + 1}) == B.MEBPTT_ERR_ARG, k
+    assert _scan(batch=70000) == B.MEBPTT_ERR_UNSUPPORTED
+    d = B.make_scan_desc(2, 24, 16, 1, 10, "bf16")
+    assert B.mebptt_scan_workspace_bytes(d) == 0                      # nothing to hold: one segment
+    need = B.mebptt_scan_workspace_bytes(d, True)
+    for ws, nbytes in ((None, need), (P + 64, need), (P, need - 1)):
+        assert _scan(True, ws=ws, nbytes=nbytes) == B.MEBPTT_ERR_WORKSPACE
+    d.t = 4000
+    assert B.mebptt_scan_workspace_bytes(d) > 0 and _scan(t=4000, ws=None) == B.MEBPTT_ERR_WORKSPACE
+
+
+def test_states_that_are_kept_take_what_the_spacing_says():
+    for spacing in (8, 16, 32):
+        d = B.make_scan_desc(3, 40, 10, 2, 100, "fp32", spacing=spacing)
+        assert B.mebptt_scan_kept_bytes(d) == -(-100 // spacing) * 3 * 40 * 16 * 4
+    d.spacing = 9
+    assert B.mebptt_scan_kept_bytes(d) == 0
+
+
+@pytest.mark.parametrize("kw", [
+    dict(rows=0), dict(vocabulary=0), dict(entries=0), dict(entries=1025), dict(dtype=7), dict(reserved=1), dict(temperature=0.0),
+    dict(temperature=-1.0), dict(temperature=float("nan")), dict(temperature=float("inf")), dict(scale=float("inf")), dict(scale=float("nan")),
+    dict(logits_row=99), dict(dlogits_row=99), dict(logits_row=-1), dict(p_logits=None), dict(p_indices=None), dict(p_values=None),
+    dict(p_logits=P + 1), dict(p_indices=P + 2), dict(p_values=P + 2), dict(p_weights=P + 2),
+])
+@pytest.mark.parametrize("which", ["loss", "grad", "both"])
+def test_distill_refuses(which, kw):
+    assert _distill(which, **kw) == B.MEBPTT_ERR_ARG
+
+
+def test_distill_refuses_more():
+    assert _distill("loss", p_row_loss=None) == _distill("loss", p_stats=None) == _distill("loss", p_loss=P + 2) == B.MEBPTT_ERR_ARG
+    assert _distill("grad", p_stats=None) == _distill("grad", p_dlogits=None) == _distill("grad", p_dlogits=P + 1) == B.MEBPTT_ERR_ARG
+    assert _distill("both", p_row_loss=None) == _distill("both", p_dlogits=None) == _distill("both", p_dloss=P + 1) == B.MEBPTT_ERR_ARG
+    assert _distill("both", rows=1 << 31) == B.MEBPTT_ERR_UNSUPPORTED
+
+
+def test_null_descriptors_are_refused():
+    assert B.lib.mebptt_conv_forward(*[None] * 9) == B.MEBPTT_ERR_ARG
+    assert B.lib.mebptt_conv_workspace_bytes(None) == B.lib.mebptt_scan_kept_bytes(None) == B.lib.mebptt_scan_workspace_bytes(None, 1) == 0
+    assert B.lib.mebptt_scan_forward(*[None] * 12, 0, *[None] * 4) == B.MEBPTT_ERR_ARG
+    assert B.lib.mebptt_distill_loss(*[None] * 9) == B.MEBPTT_ERR_ARG
+
+
+def test_tensors_of_another_type_or_place_are_refused():
+    import torch
+    d = B.make_conv_desc(1, 8, 2, 1, "bf16")
+    x = torch.zeros(1, 1, 8, dtype=torch.bfloat16)
+    with pytest.raises(B.MebpttError) as e:
+        B.mebptt_conv_forward(d, x, x, None, None, None, None, x, None)
+    assert e.value.status == B.MEBPTT_ERR_ARG
