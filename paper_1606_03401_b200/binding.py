@@ -440,33 +440,42 @@ def make_distill_desc(rows, vocabulary, entries, dtype, temperature=1.0, scale=1
     return mebptt_distill_desc(rows, vocabulary, entries, _dtype(dtype), 0, temperature, scale, logits_row, dlogits_row)
 
 
-_OPERANDS = {MEBPTT_BF16: ("torch.bfloat16", 2), MEBPTT_FP32: ("torch.float32", 4), MEBPTT_TF32: ("torch.float32", 4)}
+_TYPES = {}
 
 
-def _typed(name, dtype, operands, floats, ints=()):
-    """Raises where a tensor's type is not what the call takes it for (a wrong one would be read past its end)."""
-    want = _OPERANDS.get(dtype)
-    for group, kind in ((operands, want and want[0]), (floats, "torch.float32"), (ints, "torch.int32")):
+def _pointers(name, desc, operands, floats, ints=()):
+    """Addresses of the tensors, in three lists.  Raises where one's type or place is not what the call takes it for (a wrong
+    one would be read past its end)."""
+    if not _TYPES:
+        import torch
+        _TYPES.update({MEBPTT_BF16: torch.bfloat16, MEBPTT_FP32: torch.float32, MEBPTT_TF32: torch.float32, "f": torch.float32, "i": torch.int32})
+    out = []
+    for group, want in ((operands, _TYPES.get(desc.dtype)), (floats, _TYPES["f"]), (ints, _TYPES["i"])):
+        p = []
         for x in group:
-            if x is not None and not (x.is_cuda and _NAMES.get(x.dtype) == kind):
-                raise MebpttError(MEBPTT_ERR_ARG, f"{name}: a {x.dtype} tensor on {x.device} where a CUDA tensor of {kind} belongs")
+            if x is None:
+                p.append(None)
+            elif x.dtype is want and x.is_cuda:
+                p.append(x.data_ptr())
+            else:
+                raise MebpttError(MEBPTT_ERR_ARG, f"{name}: a {x.dtype} tensor on {x.device} where a CUDA tensor of {want} belongs")
+        out.append(p)
+    return out
 
 
-class _Names(dict):
-    def __missing__(self, dtype):
-        self[dtype] = str(dtype)
-        return self[dtype]
-
-    def get(self, dtype):
-        return self[dtype]
-
-
-_NAMES = _Names()
+def _room(name, what, x, need):
+    """Address and size of a buffer of bytes (0 for none); raises where it is smaller than the call takes it for."""
+    if x is None:
+        return None, 0
+    n = _nbytes(x)
+    if n < need:
+        raise MebpttError(MEBPTT_ERR_WORKSPACE, f"{name}: {what}")
+    return x.data_ptr(), n
 
 
 def mebptt_conv_forward(desc, x, w, bias, s_in, lengths, stream, y, s_out):
-    _typed("mebptt_conv_forward", desc.dtype, (x, w, s_in, y, s_out), (bias,), (lengths,))
-    st = lib.mebptt_conv_forward(C.addressof(desc), _ptr(x), _ptr(w), _ptr(bias), _ptr(s_in), _ptr(lengths), stream, _ptr(y), _ptr(s_out))
+    (x, w, s_in, y, s_out), (bias,), (lengths,) = _pointers("mebptt_conv_forward", desc, (x, w, s_in, y, s_out), (bias,), (lengths,))
+    st = lib.mebptt_conv_forward(C.addressof(desc), x, w, bias, s_in, lengths, stream, y, s_out)
     _check(st, "mebptt_conv_forward")
 
 
@@ -475,10 +484,11 @@ def mebptt_conv_workspace_bytes(desc) -> int:
 
 
 def mebptt_conv_backward(desc, x, w, bias, s_in, lengths, dy, ds_out, workspace, stream, dx, dw, dbias, ds_in):
-    _typed("mebptt_conv_backward", desc.dtype, (x, w, s_in, dy, ds_out, dx, ds_in), (bias, dw, dbias), (lengths,))
-    st = lib.mebptt_conv_backward(C.addressof(desc), _ptr(x), _ptr(w), _ptr(bias), _ptr(s_in), _ptr(lengths), _ptr(dy), _ptr(ds_out),
-                                  _ptr(workspace), _nbytes(workspace), stream, _ptr(dx), _ptr(dw), _ptr(dbias), _ptr(ds_in))
-    _check(st, "mebptt_conv_backward")
+    name = "mebptt_conv_backward"
+    (x, w, s_in, dy, ds_out, dx, ds_in), (bias, dw, dbias), (lengths,) = _pointers(
+        name, desc, (x, w, s_in, dy, ds_out, dx, ds_in), (bias, dw, dbias), (lengths,))
+    ws, nbytes = _room(name, "workspace", workspace, 0)
+    _check(lib.mebptt_conv_backward(C.addressof(desc), x, w, bias, s_in, lengths, dy, ds_out, ws, nbytes, stream, dx, dw, dbias, ds_in), name)
 
 
 def mebptt_scan_kept_bytes(desc) -> int:
@@ -490,44 +500,41 @@ def mebptt_scan_workspace_bytes(desc, backward=False) -> int:
 
 
 def mebptt_scan_forward(desc, u, delta, A, Bm, Cm, skip, z, delta_bias, s_in, lengths, workspace, stream, y, s_out, kept=None):
-    _typed("mebptt_scan_forward", desc.dtype, (u, delta, Bm, Cm, z, y), (A, skip, delta_bias, s_in, s_out), (lengths,))
-    if kept is not None and _nbytes(kept) < mebptt_scan_kept_bytes(desc):
-        raise MebpttError(MEBPTT_ERR_WORKSPACE, "mebptt_scan_forward: kept")
-    st = lib.mebptt_scan_forward(C.addressof(desc), _ptr(u), _ptr(delta), _ptr(A), _ptr(Bm), _ptr(Cm), _ptr(skip), _ptr(z),
-                                 _ptr(delta_bias), _ptr(s_in), _ptr(lengths), _ptr(workspace),
-                                 0 if workspace is None else _nbytes(workspace), stream, _ptr(y), _ptr(s_out), _ptr(kept))
-    _check(st, "mebptt_scan_forward")
+    name = "mebptt_scan_forward"
+    (u, delta, Bm, Cm, z, y), (A, skip, delta_bias, s_in, s_out), (lengths,) = _pointers(
+        name, desc, (u, delta, Bm, Cm, z, y), (A, skip, delta_bias, s_in, s_out), (lengths,))
+    ws, nbytes = _room(name, "workspace", workspace, 0)
+    kept = None if kept is None else _room(name, "kept", kept, mebptt_scan_kept_bytes(desc))[0]
+    _check(lib.mebptt_scan_forward(C.addressof(desc), u, delta, A, Bm, Cm, skip, z, delta_bias, s_in, lengths, ws, nbytes, stream, y, s_out, kept), name)
 
 
 def mebptt_scan_backward(desc, u, delta, A, Bm, Cm, skip, z, delta_bias, lengths, kept, dy, ds_out, workspace, stream, du, ddelta,
                          dA, dB, dC, dskip, dz, ddelta_bias, ds_in):
-    _typed("mebptt_scan_backward", desc.dtype, (u, delta, Bm, Cm, z, dy, du, ddelta, dB, dC, dz),
-           (A, skip, delta_bias, ds_out, dA, dskip, ddelta_bias, ds_in), (lengths,))
-    if kept is not None and _nbytes(kept) < mebptt_scan_kept_bytes(desc):
-        raise MebpttError(MEBPTT_ERR_WORKSPACE, "mebptt_scan_backward: kept")
-    st = lib.mebptt_scan_backward(C.addressof(desc), _ptr(u), _ptr(delta), _ptr(A), _ptr(Bm), _ptr(Cm), _ptr(skip), _ptr(z),
-                                  _ptr(delta_bias), _ptr(lengths), _ptr(kept), _ptr(dy), _ptr(ds_out), _ptr(workspace),
-                                  0 if workspace is None else _nbytes(workspace), stream, _ptr(du), _ptr(ddelta), _ptr(dA), _ptr(dB),
-                                  _ptr(dC), _ptr(dskip), _ptr(dz), _ptr(ddelta_bias), _ptr(ds_in))
-    _check(st, "mebptt_scan_backward")
+    name = "mebptt_scan_backward"
+    (u, delta, Bm, Cm, z, dy, du, ddelta, dB, dC, dz), (A, skip, delta_bias, ds_out, dA, dskip, ddelta_bias, ds_in), (lengths,) = _pointers(
+        name, desc, (u, delta, Bm, Cm, z, dy, du, ddelta, dB, dC, dz), (A, skip, delta_bias, ds_out, dA, dskip, ddelta_bias, ds_in), (lengths,))
+    ws, nbytes = _room(name, "workspace", workspace, 0)
+    kept = None if kept is None else _room(name, "kept", kept, mebptt_scan_kept_bytes(desc))[0]
+    _check(lib.mebptt_scan_backward(C.addressof(desc), u, delta, A, Bm, Cm, skip, z, delta_bias, lengths, kept, dy, ds_out, ws, nbytes, stream,
+                                    du, ddelta, dA, dB, dC, dskip, dz, ddelta_bias, ds_in), name)
 
 
 def mebptt_distill_loss(desc, logits, indices, values, weights, stream, loss, row_loss, row_stats):
-    _typed("mebptt_distill_loss", desc.dtype, (logits,), (values, weights, loss, row_loss, row_stats), (indices,))
-    st = lib.mebptt_distill_loss(C.addressof(desc), _ptr(logits), _ptr(indices), _ptr(values), _ptr(weights), stream, _ptr(loss),
-                                 _ptr(row_loss), _ptr(row_stats))
-    _check(st, "mebptt_distill_loss")
+    name = "mebptt_distill_loss"
+    (logits,), (values, weights, loss, row_loss, row_stats), (indices,) = _pointers(
+        name, desc, (logits,), (values, weights, loss, row_loss, row_stats), (indices,))
+    _check(lib.mebptt_distill_loss(C.addressof(desc), logits, indices, values, weights, stream, loss, row_loss, row_stats), name)
 
 
 def mebptt_distill_grad(desc, logits, indices, values, weights, row_stats, dloss, stream, dlogits):
-    _typed("mebptt_distill_grad", desc.dtype, (logits, dlogits), (values, weights, row_stats, dloss), (indices,))
-    st = lib.mebptt_distill_grad(C.addressof(desc), _ptr(logits), _ptr(indices), _ptr(values), _ptr(weights), _ptr(row_stats),
-                                 _ptr(dloss), stream, _ptr(dlogits))
-    _check(st, "mebptt_distill_grad")
+    name = "mebptt_distill_grad"
+    (logits, dlogits), (values, weights, row_stats, dloss), (indices,) = _pointers(
+        name, desc, (logits, dlogits), (values, weights, row_stats, dloss), (indices,))
+    _check(lib.mebptt_distill_grad(C.addressof(desc), logits, indices, values, weights, row_stats, dloss, stream, dlogits), name)
 
 
 def mebptt_distill_loss_grad(desc, logits, indices, values, weights, dloss, stream, loss, row_loss, dlogits):
-    _typed("mebptt_distill_loss_grad", desc.dtype, (logits, dlogits), (values, weights, dloss, loss, row_loss), (indices,))
-    st = lib.mebptt_distill_loss_grad(C.addressof(desc), _ptr(logits), _ptr(indices), _ptr(values), _ptr(weights), _ptr(dloss), stream,
-                                      _ptr(loss), _ptr(row_loss), _ptr(dlogits))
-    _check(st, "mebptt_distill_loss_grad")
+    name = "mebptt_distill_loss_grad"
+    (logits, dlogits), (values, weights, dloss, loss, row_loss), (indices,) = _pointers(
+        name, desc, (logits, dlogits), (values, weights, dloss, loss, row_loss), (indices,))
+    _check(lib.mebptt_distill_loss_grad(C.addressof(desc), logits, indices, values, weights, dloss, stream, loss, row_loss, dlogits), name)

@@ -1,8 +1,8 @@
 // Short causal convolution, channel by channel, with a state for token-by-token use; forward and backward.
 //
-// A thread has `C` neighbouring channels of one row (8 or 16 bytes of them) and walks a run of time steps with the last
+// A thread has `C` neighbouring channels of one row and walks a run of time steps with the last
 // width - 1 inputs in registers, so that every input is loaded once (and width - 1 of them a second time where a run begins).
-// Loads of U steps are issued together.  Bound by memory: 2 accesses an element forward, 3 backward.
+// Loads of U steps are issued together, while the U steps before them are computed.  Bound by memory: 2 accesses an element forward, 3 backward.
 #include <cuda_runtime.h>
 
 #include <cstdint>
@@ -17,6 +17,7 @@ namespace seq {
 
 namespace {
 
+constexpr int C = 4;          // channels of a thread: taps, inputs, and backward also gradients and sums, are held for each
 constexpr int U = 4;          // steps whose loads are issued together
 constexpr int ROWS = 8;       // runs of a block that share their channels
 constexpr int COLS = 32;      // groups of channels of a block
@@ -34,7 +35,7 @@ struct ConvArgs {
 };
 
 // The state of row b as float [W - 1][C]; zeros without one.
-template <int W, int C, class T>
+template <int W, class T>
 __device__ __forceinline__ void load_state(const T* s, int b, int D, int c0, int n, bool whole, float (&f)[W > 1 ? W - 1 : 1][C]) {
 #pragma unroll
   for (int i = 0; i < W - 1; ++i) {
@@ -48,10 +49,10 @@ __device__ __forceinline__ void load_state(const T* s, int b, int D, int c0, int
 }
 
 // What precedes step k0 of a row: inputs, or the state before step 0 (k0 = 0 or k0 >= W - 1).  Steps at or past n are zeros.
-template <int W, int C, class T>
+template <int W, class T>
 __device__ __forceinline__ void load_before(const ConvArgs& a, const T* x, int b, int k0, int n, int c0, int nc, float (&f)[W > 1 ? W - 1 : 1][C]) {
   if (k0 == 0) {
-    load_state<W, C>((const T*)a.s_in, b, a.channels, c0, nc, nc == C && a.aligned_s, f);
+    load_state<W, T>((const T*)a.s_in, b, a.channels, c0, nc, nc == C && a.aligned_s, f);
     return;
   }
 #pragma unroll
@@ -61,7 +62,7 @@ __device__ __forceinline__ void load_before(const ConvArgs& a, const T* x, int b
   }
 }
 
-template <class T, int C, int W>
+template <class T, int W>
 __global__ void __launch_bounds__(COLS* ROWS) conv_fwd(const ConvArgs a) {
   const int group = blockIdx.y * COLS + threadIdx.x;
   const int64_t item = (int64_t)blockIdx.x * ROWS + threadIdx.y;    // run of a row: rows of one run are neighbours
@@ -75,7 +76,7 @@ __global__ void __launch_bounds__(COLS* ROWS) conv_fwd(const ConvArgs a) {
   const bool wx = nc == C && a.aligned_x, wy = nc == C && a.aligned_y;
 
   float win[W > 1 ? W - 1 : 1][C];
-  load_before<W, C>(a, x, b, k0, n, c0, nc, win);
+  load_before<W, T>(a, x, b, k0, n, c0, nc, win);
   if (W > 1 && r == 0 && a.s_out) {
     // the last W - 1 of state and inputs; this thread alone reads and writes this part of the state
     T* so = (T*)a.s_out + (int64_t)b * (W - 1) * a.channels + c0;
@@ -106,10 +107,16 @@ __global__ void __launch_bounds__(COLS* ROWS) conv_fwd(const ConvArgs a) {
 #pragma unroll
     for (int j = 0; j < W; ++j) w[j][c] = c < nc ? to_f<T>(((const T*)a.w)[(int64_t)(c0 + c) * W + j]) : 0.f;
   }
-  for (int k = k0; k < k1; k += U) {
-    Raw<T, C> raw[U];
+  Raw<T, C> raw[U], next[U];
+  auto load = [&](Raw<T, C>(&to)[U], int k) {
 #pragma unroll
-    for (int i = 0; i < U; ++i) raw[i] = k + i < n && k + i < k1 ? load_raw<C>(x + (int64_t)(k + i) * a.px.step, nc, wx) : raw_zeros<T, C>();
+    for (int i = 0; i < U; ++i) to[i] = k + i < n && k + i < k1 ? load_raw<C>(x + (int64_t)(k + i) * a.px.step, nc, wx) : raw_zeros<T, C>();
+  };
+  load(next, k0);
+  for (int k = k0; k < k1; k += U) {
+#pragma unroll
+    for (int i = 0; i < U; ++i) raw[i] = next[i];
+    load(next, k + U);
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       float v[C], p[C];
@@ -132,7 +139,7 @@ __global__ void __launch_bounds__(COLS* ROWS) conv_fwd(const ConvArgs a) {
 
 // dext_e = sum_j w[j] dp_{e - j} (+ ds_out where e >= n) over positions e = k + W - 1 of state and inputs together: the walk over k
 // emits position k, the input of step k - W + 1 (or the state's, for k < W - 1 in a row's first run).
-template <class T, int C, int W>
+template <class T, int W>
 __global__ void __launch_bounds__(COLS* ROWS) conv_bwd(const ConvArgs a) {
   __shared__ float red[ROWS][COLS * C];
   const int group = blockIdx.y * COLS + threadIdx.x;
@@ -160,21 +167,27 @@ __global__ void __launch_bounds__(COLS* ROWS) conv_bwd(const ConvArgs a) {
       for (int j = 0; j < W; ++j) w[j][c] = c < nc ? to_f<T>(((const T*)a.w)[(int64_t)(c0 + c) * W + j]) : 0.f;
     }
     float win[W > 1 ? W - 1 : 1][C], dp[W][C];     // dp[j]: that of step k - j
-    load_before<W, C>(a, x, b, k0, n, c0, nc, win);
+    load_before<W, T>(a, x, b, k0, n, c0, nc, win);
 #pragma unroll
     for (int j = 0; j < W; ++j)
 #pragma unroll
       for (int c = 0; c < C; ++c) dp[j][c] = 0.f;
 
     const int end = k1 + W - 1;                    // steps k1 .. end - 1 are the next run's: only their dp is needed
-    for (int k = k0; k < end; k += U) {
-      Raw<T, C> raw[U], rdy[U];
+    Raw<T, C> raw[U], rdy[U], next[U], ndy[U];
+    auto load = [&](int k) {
 #pragma unroll
       for (int i = 0; i < U; ++i) {
         const bool in = k + i < n && k + i < end;
-        raw[i] = in ? load_raw<C>(x + (int64_t)(k + i) * a.px.step, nc, wx) : raw_zeros<T, C>();
-        rdy[i] = in ? load_raw<C>(dy + (int64_t)(k + i) * a.py.step, nc, wy) : raw_zeros<T, C>();
+        next[i] = in ? load_raw<C>(x + (int64_t)(k + i) * a.px.step, nc, wx) : raw_zeros<T, C>();
+        ndy[i] = in ? load_raw<C>(dy + (int64_t)(k + i) * a.py.step, nc, wy) : raw_zeros<T, C>();
       }
+    };
+    load(k0);
+    for (int k = k0; k < end; k += U) {
+#pragma unroll
+      for (int i = 0; i < U; ++i) { raw[i] = next[i]; rdy[i] = ndy[i]; }
+      load(k + U);
 #pragma unroll
       for (int i = 0; i < U; ++i) {
         const int kk = k + i;
@@ -261,24 +274,19 @@ __global__ void __launch_bounds__(256) conv_sums(const float* part, int parts, i
   else if (dbias) dbias[d] = s;
 }
 
-// Channels of a thread: 16 bytes of them, but 8 bytes where bfloat16 would leave too few registers (taps, inputs, and backward
-// also gradients and sums, are held for each channel).
-constexpr bool wide(int dtype, int width, bool back) { return dtype == MEBPTT_BF16 && !back && width <= 4; }
-
 struct ConvPlan {
-  int C, groups, run, runs;
+  int groups, run, runs;
   int64_t items;
   unsigned blocks, cols;   // of runs, of channels
 };
 
 // Steps of a run: as many as leave every SM a thousand threads, 8 at least (a run begins with width - 1 inputs that its
-// neighbour also loads) and 64 at most.
-bool conv_plan(const mebptt_conv_desc* d, bool back, ConvPlan& p) {
-  p.C = wide(d->dtype, d->width, back) ? 8 : 4;
-  p.groups = (d->channels + p.C - 1) / p.C;
+// neighbour also loads) and 32 at most (blocks of several waves even the SMs out).
+bool conv_plan(const mebptt_conv_desc* d, ConvPlan& p) {
+  p.groups = (d->channels + C - 1) / C;
   const int64_t threads = (int64_t)148 * 1024;
   int64_t run = (int64_t)p.groups * d->batch * d->t / threads;
-  run = run < 8 ? 8 : run > 64 ? 64 : run / 4 * 4;
+  run = run < 8 ? 8 : run > 32 ? 32 : run / 4 * 4;
   p.runs = (int)((d->t + run - 1) / run);
   p.run = (int)run;
   p.items = (int64_t)d->batch * p.runs;
@@ -298,8 +306,8 @@ bool conv_check(const mebptt_conv_desc* d, Places& px, Places& py) {
 template <class T, int W>
 void conv_launch(bool back, const ConvPlan& p, const ConvArgs& a, cudaStream_t s) {
   const dim3 grid(p.blocks, p.cols), block(COLS, ROWS);
-  if (back) conv_bwd<T, 4, W><<<grid, block, 0, counted(s)>>>(a);
-  else conv_fwd<T, sizeof(T) == 2 && W <= 4 ? 8 : 4, W><<<grid, block, 0, counted(s)>>>(a);
+  if (back) conv_bwd<T, W><<<grid, block, 0, counted(s)>>>(a);
+  else conv_fwd<T, W><<<grid, block, 0, counted(s)>>>(a);
 }
 template <class T>
 void conv_launch(int width, bool back, const ConvPlan& p, const ConvArgs& a, cudaStream_t s) {
@@ -326,9 +334,9 @@ int conv_run(const mebptt_conv_desc* d, const ConvPlan& p, const Places& px, con
   a.batch = d->batch; a.channels = d->channels; a.t = (int)d->t; a.run = p.run; a.runs = p.runs; a.groups = p.groups;
   a.silu = d->flags & MEBPTT_CONV_SILU;
   if (d->width == 1) { a.s_in = a.ds_out = nullptr; a.s_out = a.ds_in = nullptr; }
-  a.aligned_x = aligned(a.x, px, p.C, e) && aligned(a.dx, px, p.C, e);
-  a.aligned_y = aligned(back ? a.dy : a.y, py, p.C, e);
-  a.aligned_s = aligned(a.s_in, state, p.C, e) && aligned(a.s_out, state, p.C, e) && aligned(a.ds_in, state, p.C, e) && aligned(a.ds_out, state, p.C, e);
+  a.aligned_x = aligned(a.x, px, C, e) && aligned(a.dx, px, C, e);
+  a.aligned_y = aligned(back ? a.dy : a.y, py, C, e);
+  a.aligned_s = aligned(a.s_in, state, C, e) && aligned(a.s_out, state, C, e) && aligned(a.ds_in, state, C, e) && aligned(a.ds_out, state, C, e);
   if (d->dtype == MEBPTT_BF16) conv_launch<bf16>(d->width, back, p, a, s);
   else conv_launch<float>(d->width, back, p, a, s);
   return cudaGetLastError() == cudaSuccess ? MEBPTT_OK : MEBPTT_ERR_CUDA;
@@ -348,7 +356,7 @@ int mebptt_conv_forward(const mebptt_conv_desc* desc, const void* x, const void*
   Places px, py;
   ConvPlan p;
   if (!conv_check(desc, px, py) || !x || !w || !y) return MEBPTT_ERR_ARG;
-  if (!conv_plan(desc, false, p)) return MEBPTT_ERR_UNSUPPORTED;
+  if (!conv_plan(desc, p)) return MEBPTT_ERR_UNSUPPORTED;
   ConvArgs a = {};
   a.x = x; a.w = w; a.bias = bias; a.s_in = s_in; a.lengths = lengths; a.y = y; a.s_out = s_out;
   return conv_run(desc, p, px, py, a, false, (cudaStream_t)stream);
@@ -357,7 +365,7 @@ int mebptt_conv_forward(const mebptt_conv_desc* desc, const void* x, const void*
 size_t mebptt_conv_workspace_bytes(const mebptt_conv_desc* desc) {
   Places px, py;
   ConvPlan p;
-  if (!conv_check(desc, px, py) || !conv_plan(desc, true, p)) return 0;
+  if (!conv_check(desc, px, py) || !conv_plan(desc, p)) return 0;
   return (size_t)p.blocks * (desc->width + 1) * desc->channels * sizeof(float);
 }
 
@@ -367,7 +375,7 @@ int mebptt_conv_backward(const mebptt_conv_desc* desc, const void* x, const void
   Places px, py;
   ConvPlan p;
   if (!conv_check(desc, px, py) || !x || !w || !dy || !dx || !dw || !natural(dw, 4) || !natural(dbias, 4)) return MEBPTT_ERR_ARG;
-  if (!conv_plan(desc, true, p)) return MEBPTT_ERR_UNSUPPORTED;
+  if (!conv_plan(desc, p)) return MEBPTT_ERR_UNSUPPORTED;
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < mebptt_conv_workspace_bytes(desc))
     return MEBPTT_ERR_WORKSPACE;
   ConvArgs a = {};

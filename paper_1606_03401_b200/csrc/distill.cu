@@ -15,6 +15,7 @@
 #include <cfloat>
 #include <cstdint>
 
+#include "distill.hpp"
 #include "launch.hpp"
 #include "mebptt.h"
 #include "seq.hpp"
@@ -29,17 +30,6 @@ namespace {
 
 constexpr int PER_THREAD = 32;          // logits of a thread
 constexpr int MAX_THREADS = 512, MAX_CLUSTER = 8, MAX_ENTRIES = 1024;
-
-struct DistillArgs {
-  const void* logits; const int32_t* indices; const float* values; const float* weights;
-  const float* dloss; float* row_loss; float* row_stats; const float* stats_in;
-  void* dlogits;
-  int64_t row, drow;                    // elements between rows
-  int vocabulary, entries;
-  float T, scale;
-  int gradient;                         // dlogits is wanted
-  int same_phase;                       // logits and dlogits begin at the same place within 16 bytes, in every row
-};
 
 // Reductions over the block; `red` holds 32 floats for each of the values.
 __device__ __forceinline__ float warp_max(float v) {
@@ -315,15 +305,22 @@ cudaError_t launch(const DistillArgs& a, int64_t rows, int cluster, int threads,
   return cluster > 1 ? cudaLaunchKernelEx(&cfg, distill_kernel<T, WHOLE, true>, a) : cudaLaunchKernelEx(&cfg, distill_kernel<T, WHOLE, false>, a);
 }
 
+int finish(cudaError_t st, const DistillArgs& a, const mebptt_distill_desc* d, float* loss, cudaStream_t s) {
+  if (st == cudaSuccess && loss) distill_total<<<1, 1024, 0, counted(s)>>>(a.row_loss, d->rows, d->scale, loss);
+  return cudaGetLastError() == cudaSuccess && st == cudaSuccess ? MEBPTT_OK : MEBPTT_ERR_CUDA;
+}
+
 int run(const mebptt_distill_desc* d, DistillArgs& a, float* loss, cudaStream_t s) {
   const size_t e = d->dtype == MEBPTT_BF16 ? 2 : 4;
   const int VE = (int)(16 / e);
   a.row = d->logits_row ? d->logits_row : d->vocabulary;
   a.drow = d->dlogits_row ? d->dlogits_row : d->vocabulary;
-  a.vocabulary = d->vocabulary; a.entries = d->entries; a.T = d->temperature; a.scale = d->scale;
+  a.rows = d->rows; a.vocabulary = d->vocabulary; a.entries = d->entries; a.T = d->temperature; a.scale = d->scale;
   a.same_phase = a.gradient && !((reinterpret_cast<uintptr_t>(a.logits) - reinterpret_cast<uintptr_t>(a.dlogits)) & 15) && (d->rows == 1 || !((a.row - a.drow) * (int64_t)e & 15));
   // blocks of a row: so many that its logits fit their registers, and twice as many while a third of the SMs' places is not
   // taken and a block keeps 2048 logits
+  cudaError_t st;
+  if (distill_ring(a, d->dtype == MEBPTT_BF16, s, st)) return finish(st, a, d, loss, s);
   const int64_t pieces = ((int64_t)VE - 1 + d->vocabulary + VE - 1) / VE;
   const int64_t most = (int64_t)MAX_THREADS * PER_THREAD / VE;
   int cluster = 1;
@@ -333,11 +330,9 @@ int run(const mebptt_distill_desc* d, DistillArgs& a, float* loss, cudaStream_t 
   int64_t threads = (share + PER_THREAD / VE - 1) / (PER_THREAD / VE);
   threads = threads > MAX_THREADS ? MAX_THREADS : (threads + 31) / 32 * 32;
   if (d->rows * cluster >= ((int64_t)1 << 31)) return MEBPTT_ERR_UNSUPPORTED;
-  cudaError_t st;
   if (d->dtype == MEBPTT_BF16) st = whole ? launch<bf16, true>(a, d->rows, cluster, (int)threads, s) : launch<bf16, false>(a, d->rows, cluster, (int)threads, s);
   else st = whole ? launch<float, true>(a, d->rows, cluster, (int)threads, s) : launch<float, false>(a, d->rows, cluster, (int)threads, s);
-  if (st == cudaSuccess && loss) distill_total<<<1, 1024, 0, counted(s)>>>(a.row_loss, d->rows, d->scale, loss);
-  return cudaGetLastError() == cudaSuccess && st == cudaSuccess ? MEBPTT_OK : MEBPTT_ERR_CUDA;
+  return finish(st, a, d, loss, s);
 }
 
 bool check(const mebptt_distill_desc* d, const void* logits, const int32_t* indices, const float* values, const float* weights) {
