@@ -17,7 +17,9 @@ namespace seq {
 
 namespace {
 
-constexpr int C = 4;          // channels of a thread: taps, inputs, and backward also gradients and sums, are held for each
+constexpr int FWD = 4;        // channels of a thread: taps, inputs, and backward also gradients and sums, are held for each
+template <class T>
+constexpr int BWD = sizeof(T) == 2 ? 4 : 2;
 constexpr int U = 4;          // steps whose loads are issued together
 constexpr int ROWS = 8;       // runs of a block that share their channels
 constexpr int COLS = 32;      // groups of channels of a block
@@ -30,157 +32,159 @@ struct ConvArgs {
   Places px, py;
   int batch, channels, t, run, runs;     // steps of a run, runs of a row
   int groups;                            // of C channels
-  int aligned_x, aligned_y, aligned_s;   // groups that are whole can be loaded as one
   int silu;
 };
 
-// The state of row b as float [W - 1][C]; zeros without one.
-template <int W, class T>
-__device__ __forceinline__ void load_state(const T* s, int b, int D, int c0, int n, bool whole, float (&f)[W > 1 ? W - 1 : 1][C]) {
-#pragma unroll
-  for (int i = 0; i < W - 1; ++i) {
-    if (s) {
-      unpack<C>(load_raw<C>(s + ((int64_t)b * (W - 1) + i) * D + c0, n, whole), f[i]);
-    } else {
-#pragma unroll
-      for (int c = 0; c < C; ++c) f[i][c] = 0.f;
-    }
-  }
-}
+// `n` of the C channels at p, as pairs.  VEC: all of them, as one.
+template <int C, bool VEC, class T>
+__device__ __forceinline__ Raw<T, C> get(const T* p, int n) { return load_raw<C>(p, n, VEC); }
+template <int C, bool VEC, class T>
+__device__ __forceinline__ void put(T* p, const pair (&f)[C / 2], int n) { store_pairs<C>(p, f, n, VEC); }
 
-// What precedes step k0 of a row: inputs, or the state before step 0 (k0 = 0 or k0 >= W - 1).  Steps at or past n are zeros.
-template <int W, class T>
-__device__ __forceinline__ void load_before(const ConvArgs& a, const T* x, int b, int k0, int n, int c0, int nc, float (&f)[W > 1 ? W - 1 : 1][C]) {
-  if (k0 == 0) {
-    load_state<W, T>((const T*)a.s_in, b, a.channels, c0, nc, nc == C && a.aligned_s, f);
-    return;
-  }
+// The last W - 1 inputs before step k0 of a row: inputs, or the state before step 0 (k0 = 0, or k0 >= W - 1).  Zeros at or past step n.
+template <int C, int W, bool VEC, class T>
+__device__ __forceinline__ void load_before(const ConvArgs& a, const T* x, int b, int k0, int n, int c0, int nc, pair (&f)[W > 1 ? W - 1 : 1][C / 2]) {
 #pragma unroll
   for (int i = 0; i < W - 1; ++i) {
     const int k = k0 - (W - 1) + i;
-    unpack<C>(k < n ? load_raw<C>(x + (int64_t)k * a.px.step, nc, nc == C && a.aligned_x) : raw_zeros<T, C>(), f[i]);
+    Raw<T, C> r = raw_zeros<T, C>();
+    if (k0 == 0) {
+      if (a.s_in) r = get<C, VEC>((const T*)a.s_in + ((int64_t)b * (W - 1) + i) * a.channels + c0, nc);
+    } else if (k < n) {
+      r = get<C, VEC>(x + (int64_t)k * a.px.step, nc);
+    }
+    unpack_pairs<C>(r, f[i]);
+  }
+}
+template <int C, int W, class T>
+__device__ __forceinline__ void load_taps(const ConvArgs& a, int c0, int nc, pair (&w)[W][C / 2], pair (&bias)[C / 2]) {
+#pragma unroll
+  for (int c = 0; c < C; c += 2) {
+    const bool one = c < nc, two = c + 1 < nc;
+    bias[c / 2] = pack2(a.bias && one ? a.bias[c0 + c] : 0.f, a.bias && two ? a.bias[c0 + c + 1] : 0.f);
+    const T* t = (const T*)a.w + (int64_t)(c0 + c) * W;
+#pragma unroll
+    for (int j = 0; j < W; ++j) w[j][c / 2] = pack2(one ? to_f<T>(t[j]) : 0.f, two ? to_f<T>(t[W + j]) : 0.f);
   }
 }
 
-template <class T, int W>
+template <class T, int C, int W, bool VEC>
 __global__ void __launch_bounds__(COLS* ROWS) conv_fwd(const ConvArgs a) {
+  constexpr int P = C / 2, B = W > 1 ? W - 1 : 1;
   const int group = blockIdx.y * COLS + threadIdx.x;
   const int64_t item = (int64_t)blockIdx.x * ROWS + threadIdx.y;    // run of a row: rows of one run are neighbours
   if (group >= a.groups || item >= (int64_t)a.batch * a.runs) return;
   const int b = (int)(item % a.batch), r = (int)(item / a.batch);
   const int c0 = group * C, nc = min(C, a.channels - c0);
   const int n = row_steps(a.lengths, b, a.t);
-  const int k0 = r * a.run, k1 = min(k0 + a.run, a.t);
+  const int k0 = r * a.run, k1 = min(k0 + a.run, a.t), live = max(k0, min(k1, n));      // steps k0 .. live - 1 are the row's
   const T* x = (const T*)a.x + (int64_t)b * a.px.row + c0;
-  T* y = (T*)a.y + (int64_t)b * a.py.row + c0;
-  const bool wx = nc == C && a.aligned_x, wy = nc == C && a.aligned_y;
+  T* y = (T*)a.y + (int64_t)b * a.py.row + c0 + (int64_t)k0 * a.py.step;
 
-  float win[W > 1 ? W - 1 : 1][C];
-  load_before<W, T>(a, x, b, k0, n, c0, nc, win);
+  pair win[B][P];
+  load_before<C, W, VEC>(a, x, b, k0, n, c0, nc, win);
   if (W > 1 && r == 0 && a.s_out) {
     // the last W - 1 of state and inputs; this thread alone reads and writes this part of the state
-    T* so = (T*)a.s_out + (int64_t)b * (W - 1) * a.channels + c0;
-    const bool ws = nc == C && a.aligned_s;
-    float out[W > 1 ? W - 1 : 1][C];
+    pair out[B][P];
 #pragma unroll
     for (int i = 0; i < W - 1; ++i) {
       const int k = n - (W - 1) + i;
       if (k >= 0) {
-        unpack<C>(load_raw<C>(x + (int64_t)k * a.px.step, nc, wx), out[i]);
+        unpack_pairs<C>(get<C, VEC>(x + (int64_t)k * a.px.step, nc), out[i]);
       } else {
 #pragma unroll
         for (int j = 0; j < W - 1; ++j)
           if (j == n + i) {
 #pragma unroll
-            for (int c = 0; c < C; ++c) out[i][c] = win[j][c];
+            for (int c = 0; c < P; ++c) out[i][c] = win[j][c];
           }
       }
     }
+    T* const so = (T*)a.s_out + (int64_t)b * (W - 1) * a.channels + c0;
 #pragma unroll
-    for (int i = 0; i < W - 1; ++i) store_n<C>(so + (int64_t)i * a.channels, out[i], nc, ws);
+    for (int i = 0; i < W - 1; ++i) put<C, VEC>(so + (int64_t)i * a.channels, out[i], nc);
   }
 
-  float w[W][C], bias[C];
-#pragma unroll
-  for (int c = 0; c < C; ++c) {
-    bias[c] = a.bias && c < nc ? a.bias[c0 + c] : 0.f;
-#pragma unroll
-    for (int j = 0; j < W; ++j) w[j][c] = c < nc ? to_f<T>(((const T*)a.w)[(int64_t)(c0 + c) * W + j]) : 0.f;
-  }
+  pair w[W][P], bias[P];
+  load_taps<C, W, T>(a, c0, nc, w, bias);
+  const T* next_x = x + (int64_t)k0 * a.px.step;
   Raw<T, C> raw[U], next[U];
-  auto load = [&](Raw<T, C>(&to)[U], int k) {
-#pragma unroll
-    for (int i = 0; i < U; ++i) to[i] = k + i < n && k + i < k1 ? load_raw<C>(x + (int64_t)(k + i) * a.px.step, nc, wx) : raw_zeros<T, C>();
-  };
-  load(next, k0);
-  for (int k = k0; k < k1; k += U) {
-#pragma unroll
-    for (int i = 0; i < U; ++i) raw[i] = next[i];
-    load(next, k + U);
+  auto load = [&](int k) {
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-      float v[C], p[C];
-      unpack<C>(raw[i], v);
+      next[i] = k + i < live ? get<C, VEC>(next_x, nc) : raw_zeros<T, C>();
+      next_x += a.px.step;
+    }
+  };
+  load(k0);
+  for (int k = k0; k < live; k += U) {
 #pragma unroll
-      for (int c = 0; c < C; ++c) {
-        p[c] = fmaf(w[W - 1][c], v[c], bias[c]);
+    for (int i = 0; i < U; ++i) raw[i] = next[i];
+    load(k + U);
 #pragma unroll
-        for (int j = 0; j < W - 1; ++j) p[c] = fmaf(w[j][c], win[j][c], p[c]);
-        if (a.silu) p[c] *= sigmoid(p[c]);
-        if (k + i >= n) p[c] = 0.f;
+    for (int i = 0; i < U; ++i) {
+      pair v[P], p[P];
+      unpack_pairs<C>(raw[i], v);
+#pragma unroll
+      for (int c = 0; c < P; ++c) {
+        p[c] = fma2(w[W - 1][c], v[c], bias[c]);
+#pragma unroll
+        for (int j = 0; j < W - 1; ++j) p[c] = fma2(w[j][c], win[j][c], p[c]);
+        if (a.silu) p[c] = mul2(p[c], sigmoid2(p[c]));
 #pragma unroll
         for (int j = 0; j + 1 < W - 1; ++j) win[j][c] = win[j + 1][c];
-        if (W > 1) win[W - 2 < 0 ? 0 : W - 2][c] = v[c];
+        if (W > 1) win[B - 1][c] = v[c];
       }
-      if (k + i < k1) store_n<C>(y + (int64_t)(k + i) * a.py.step, p, nc, wy);
+      if (k + i < live) put<C, VEC>(y, p, nc);
+      y += a.py.step;
     }
   }
+  const pair zero[P] = {};
+  y = (T*)a.y + (int64_t)b * a.py.row + c0;
+  for (int k = live; k < k1; ++k) put<C, VEC>(y + (int64_t)k * a.py.step, zero, nc);
 }
 
 // dext_e = sum_j w[j] dp_{e - j} (+ ds_out where e >= n) over positions e = k + W - 1 of state and inputs together: the walk over k
 // emits position k, the input of step k - W + 1 (or the state's, for k < W - 1 in a row's first run).
-template <class T, int W>
-__global__ void __launch_bounds__(COLS* ROWS) conv_bwd(const ConvArgs a) {
+template <class T, int C, int W, bool VEC>
+__global__ void __launch_bounds__(COLS* ROWS, W <= 4 ? 2 : 1) conv_bwd(const ConvArgs a) {
+  constexpr int P = C / 2, B = W > 1 ? W - 1 : 1;
   __shared__ float red[ROWS][COLS * C];
   const int group = blockIdx.y * COLS + threadIdx.x;
   const int64_t item = (int64_t)blockIdx.x * ROWS + threadIdx.y;
-  float dw[W + 1][C];            // the last one: bias
+  pair dw[W + 1][P];             // the last one: bias
 #pragma unroll
   for (int j = 0; j <= W; ++j)
 #pragma unroll
-    for (int c = 0; c < C; ++c) dw[j][c] = 0.f;
+    for (int c = 0; c < P; ++c) dw[j][c] = 0;
 
   if (group < a.groups && item < (int64_t)a.batch * a.runs) {
     const int b = (int)(item % a.batch), r = (int)(item / a.batch);
     const int c0 = group * C, nc = min(C, a.channels - c0);
     const int n = row_steps(a.lengths, b, a.t);
     const int k0 = r * a.run, k1 = min(k0 + a.run, a.t);
-    const T* x = (const T*)a.x + (int64_t)b * a.px.row + c0;
-    const T* dy = (const T*)a.dy + (int64_t)b * a.py.row + c0;
-    T* dx = (T*)a.dx + (int64_t)b * a.px.row + c0;
-    const bool wx = nc == C && a.aligned_x, wy = nc == C && a.aligned_y, ws = nc == C && a.aligned_s;
-    float w[W][C], bias[C];
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-      bias[c] = a.bias && c < nc ? a.bias[c0 + c] : 0.f;
-#pragma unroll
-      for (int j = 0; j < W; ++j) w[j][c] = c < nc ? to_f<T>(((const T*)a.w)[(int64_t)(c0 + c) * W + j]) : 0.f;
-    }
-    float win[W > 1 ? W - 1 : 1][C], dp[W][C];     // dp[j]: that of step k - j
-    load_before<W, T>(a, x, b, k0, n, c0, nc, win);
+    const T* const x = (const T*)a.x + (int64_t)b * a.px.row + c0;
+    T* dx = (T*)a.dx + (int64_t)b * a.px.row + c0 + (int64_t)(k0 - (W - 1)) * a.px.step;     // of position k0
+    pair w[W][P], bias[P], win[B][P], dp[W][P];    // dp[j]: that of step k - j
+    load_taps<C, W, T>(a, c0, nc, w, bias);
+    load_before<C, W, VEC>(a, x, b, k0, n, c0, nc, win);
 #pragma unroll
     for (int j = 0; j < W; ++j)
 #pragma unroll
-      for (int c = 0; c < C; ++c) dp[j][c] = 0.f;
+      for (int c = 0; c < P; ++c) dp[j][c] = 0;
 
-    const int end = k1 + W - 1;                    // steps k1 .. end - 1 are the next run's: only their dp is needed
+    const int end = k1 + W - 1, live = min(end, n); // steps k1 .. end - 1 are the next run's: only their dp is needed
+    const T* next_x = x + (int64_t)k0 * a.px.step;
+    const T* next_dy = (const T*)a.dy + (int64_t)b * a.py.row + c0 + (int64_t)k0 * a.py.step;
     Raw<T, C> raw[U], rdy[U], next[U], ndy[U];
     auto load = [&](int k) {
 #pragma unroll
       for (int i = 0; i < U; ++i) {
-        const bool in = k + i < n && k + i < end;
-        next[i] = in ? load_raw<C>(x + (int64_t)(k + i) * a.px.step, nc, wx) : raw_zeros<T, C>();
-        ndy[i] = in ? load_raw<C>(dy + (int64_t)(k + i) * a.py.step, nc, wy) : raw_zeros<T, C>();
+        const bool in = k + i < live;
+        next[i] = in ? get<C, VEC>(next_x, nc) : raw_zeros<T, C>();
+        ndy[i] = in ? get<C, VEC>(next_dy, nc) : raw_zeros<T, C>();
+        next_x += a.px.step;
+        next_dy += a.py.step;
       }
     };
     load(k0);
@@ -191,51 +195,52 @@ __global__ void __launch_bounds__(COLS* ROWS) conv_bwd(const ConvArgs a) {
 #pragma unroll
       for (int i = 0; i < U; ++i) {
         const int kk = k + i;
-        float v[C], g[C], out[C];
-        unpack<C>(raw[i], v);
-        unpack<C>(rdy[i], g);
+        pair v[P], g[P], out[P];
+        unpack_pairs<C>(raw[i], v);
+        unpack_pairs<C>(rdy[i], g);
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
+        for (int c = 0; c < P; ++c) {
           if (a.silu) {
-            float p = fmaf(w[W - 1][c], v[c], bias[c]);
+            pair p = fma2(w[W - 1][c], v[c], bias[c]);
 #pragma unroll
-            for (int j = 0; j < W - 1; ++j) p = fmaf(w[j][c], win[j][c], p);
-            g[c] *= dsilu(p, sigmoid(p));
+            for (int j = 0; j < W - 1; ++j) p = fma2(w[j][c], win[j][c], p);
+            // silu' = s (1 + p (1 - s))
+            const pair s = sigmoid2(p), rest = fma2(s, both(-1.f), both(1.f));
+            g[c] = mul2(g[c], mul2(s, fma2(p, rest, both(1.f))));
           }
-          if (kk >= n || kk >= end) g[c] = 0.f;
+          if (kk >= live) g[c] = 0;
           if (kk < k1) {
-            dw[W][c] += g[c];
-            dw[W - 1][c] = fmaf(g[c], v[c], dw[W - 1][c]);
+            dw[W][c] = add2(dw[W][c], g[c]);
+            dw[W - 1][c] = fma2(g[c], v[c], dw[W - 1][c]);
 #pragma unroll
-            for (int j = 0; j < W - 1; ++j) dw[j][c] = fmaf(g[c], win[j][c], dw[j][c]);
+            for (int j = 0; j < W - 1; ++j) dw[j][c] = fma2(g[c], win[j][c], dw[j][c]);
           }
 #pragma unroll
           for (int j = W - 1; j > 0; --j) dp[j][c] = dp[j - 1][c];
           dp[0][c] = g[c];
-          out[c] = w[0][c] * dp[0][c];
+          out[c] = mul2(w[0][c], dp[0][c]);
 #pragma unroll
-          for (int j = 1; j < W; ++j) out[c] = fmaf(w[j][c], dp[j][c], out[c]);
+          for (int j = 1; j < W; ++j) out[c] = fma2(w[j][c], dp[j][c], out[c]);
 #pragma unroll
           for (int j = 0; j + 1 < W - 1; ++j) win[j][c] = win[j + 1][c];
-          if (W > 1) win[W - 2 < 0 ? 0 : W - 2][c] = v[c];
+          if (W > 1) win[B - 1][c] = v[c];
         }
-        if (kk >= end) continue;
-        const int i_out = kk - (W - 1);            // the input that position kk belongs to; negative: the state's
-        if (i_out < k0 && !(r == 0 && a.ds_in)) continue;
-        if (W > 1 && a.ds_out && kk >= n && kk - n < W - 1) {
-          float d[C];
-          unpack<C>(load_raw<C>((const T*)a.ds_out + ((int64_t)b * (W - 1) + (kk - n)) * a.channels + c0, nc, ws), d);
+        const int at = kk - (W - 1);               // the input that position kk belongs to; negative: the state's
+        if (W > 1 && a.ds_out && kk >= n && kk - n < W - 1 && kk < end) {
+          pair d[P];
+          unpack_pairs<C>(get<C, VEC>((const T*)a.ds_out + ((int64_t)b * (W - 1) + (kk - n)) * a.channels + c0, nc), d);
 #pragma unroll
-          for (int c = 0; c < C; ++c) out[c] += d[c];
+          for (int c = 0; c < P; ++c) out[c] = add2(out[c], d[c]);
         }
-        if (i_out >= 0) {
+        if (kk < end && at >= k0) {
+          if (at >= n)
 #pragma unroll
-          for (int c = 0; c < C; ++c)
-            if (i_out >= n) out[c] = 0.f;
-          store_n<C>(dx + (int64_t)i_out * a.px.step, out, nc, wx);
-        } else {
-          store_n<C>((T*)a.ds_in + ((int64_t)b * (W - 1) + kk) * a.channels + c0, out, nc, ws);
+            for (int c = 0; c < P; ++c) out[c] = 0;
+          put<C, VEC>(dx, out, nc);
+        } else if (W > 1 && kk < end && at < 0 && a.ds_in) {
+          put<C, VEC>((T*)a.ds_in + ((int64_t)b * (W - 1) + kk) * a.channels + c0, out, nc);
         }
+        dx += a.px.step;
       }
     }
   }
@@ -245,7 +250,7 @@ __global__ void __launch_bounds__(COLS* ROWS) conv_bwd(const ConvArgs a) {
   for (int j = 0; j <= W; ++j) {
     __syncthreads();
 #pragma unroll
-    for (int c = 0; c < C; ++c) red[threadIdx.y][threadIdx.x * C + c] = dw[j][c];
+    for (int c = 0; c < P; ++c) *reinterpret_cast<float2*>(&red[threadIdx.y][threadIdx.x * C + 2 * c]) = unpack2(dw[j][c]);
     __syncthreads();
     for (int i = tid; i < COLS * C; i += COLS * ROWS) {
       const int d = blockIdx.y * COLS * C + i;
@@ -275,14 +280,15 @@ __global__ void __launch_bounds__(256) conv_sums(const float* part, int parts, i
 }
 
 struct ConvPlan {
-  int groups, run, runs;
+  int C, groups, run, runs;
   int64_t items;
   unsigned blocks, cols;   // of runs, of channels
 };
 
 // Steps of a run: as many as leave every SM a thousand threads, 8 at least (a run begins with width - 1 inputs that its
 // neighbour also loads) and 32 at most (blocks of several waves even the SMs out).
-bool conv_plan(const mebptt_conv_desc* d, ConvPlan& p) {
+bool conv_plan(const mebptt_conv_desc* d, bool back, ConvPlan& p) {
+  const int C = p.C = !back ? FWD : d->dtype == MEBPTT_BF16 ? BWD<bf16> : BWD<float>;
   p.groups = (d->channels + C - 1) / C;
   const int64_t threads = (int64_t)148 * 1024;
   int64_t run = (int64_t)p.groups * d->batch * d->t / threads;
@@ -304,22 +310,23 @@ bool conv_check(const mebptt_conv_desc* d, Places& px, Places& py) {
 }
 
 template <class T, int W>
-void conv_launch(bool back, const ConvPlan& p, const ConvArgs& a, cudaStream_t s) {
+void conv_launch(bool back, bool vec, const ConvPlan& p, const ConvArgs& a, cudaStream_t s) {
   const dim3 grid(p.blocks, p.cols), block(COLS, ROWS);
-  if (back) conv_bwd<T, W><<<grid, block, 0, counted(s)>>>(a);
-  else conv_fwd<T, W><<<grid, block, 0, counted(s)>>>(a);
+  (void)counted(s);
+  if (back) vec ? conv_bwd<T, BWD<T>, W, true><<<grid, block, 0, s>>>(a) : conv_bwd<T, BWD<T>, W, false><<<grid, block, 0, s>>>(a);
+  else vec ? conv_fwd<T, FWD, W, true><<<grid, block, 0, s>>>(a) : conv_fwd<T, FWD, W, false><<<grid, block, 0, s>>>(a);
 }
 template <class T>
-void conv_launch(int width, bool back, const ConvPlan& p, const ConvArgs& a, cudaStream_t s) {
+void conv_launch(int width, bool back, bool vec, const ConvPlan& p, const ConvArgs& a, cudaStream_t s) {
   switch (width) {
-    case 1: return conv_launch<T, 1>(back, p, a, s);
-    case 2: return conv_launch<T, 2>(back, p, a, s);
-    case 3: return conv_launch<T, 3>(back, p, a, s);
-    case 4: return conv_launch<T, 4>(back, p, a, s);
-    case 5: return conv_launch<T, 5>(back, p, a, s);
-    case 6: return conv_launch<T, 6>(back, p, a, s);
-    case 7: return conv_launch<T, 7>(back, p, a, s);
-    default: return conv_launch<T, 8>(back, p, a, s);
+    case 1: return conv_launch<T, 1>(back, vec, p, a, s);
+    case 2: return conv_launch<T, 2>(back, vec, p, a, s);
+    case 3: return conv_launch<T, 3>(back, vec, p, a, s);
+    case 4: return conv_launch<T, 4>(back, vec, p, a, s);
+    case 5: return conv_launch<T, 5>(back, vec, p, a, s);
+    case 6: return conv_launch<T, 6>(back, vec, p, a, s);
+    case 7: return conv_launch<T, 7>(back, vec, p, a, s);
+    default: return conv_launch<T, 8>(back, vec, p, a, s);
   }
 }
 
@@ -334,11 +341,16 @@ int conv_run(const mebptt_conv_desc* d, const ConvPlan& p, const Places& px, con
   a.batch = d->batch; a.channels = d->channels; a.t = (int)d->t; a.run = p.run; a.runs = p.runs; a.groups = p.groups;
   a.silu = d->flags & MEBPTT_CONV_SILU;
   if (d->width == 1) { a.s_in = a.ds_out = nullptr; a.s_out = a.ds_in = nullptr; }
-  a.aligned_x = aligned(a.x, px, C, e) && aligned(a.dx, px, C, e);
-  a.aligned_y = aligned(back ? a.dy : a.y, py, C, e);
-  a.aligned_s = aligned(a.s_in, state, C, e) && aligned(a.s_out, state, C, e) && aligned(a.ds_in, state, C, e) && aligned(a.ds_out, state, C, e);
-  if (d->dtype == MEBPTT_BF16) conv_launch<bf16>(d->width, back, p, a, s);
-  else conv_launch<float>(d->width, back, p, a, s);
+  // whole groups of channels, on their own size's boundaries: loaded and stored as one
+  const void* const xs[] = {a.x, a.dx};
+  const void* const ys[] = {a.y, a.dy};
+  const void* const ss[] = {a.s_in, a.s_out, a.ds_in, a.ds_out};
+  bool vec = d->channels % p.C == 0;
+  for (const void* q : xs) vec = vec && aligned(q, px, p.C, e);
+  for (const void* q : ys) vec = vec && aligned(q, py, p.C, e);
+  for (const void* q : ss) vec = vec && aligned(q, state, p.C, e);
+  if (d->dtype == MEBPTT_BF16) conv_launch<bf16>(d->width, back, vec, p, a, s);
+  else conv_launch<float>(d->width, back, vec, p, a, s);
   return cudaGetLastError() == cudaSuccess ? MEBPTT_OK : MEBPTT_ERR_CUDA;
 }
 
@@ -356,7 +368,7 @@ int mebptt_conv_forward(const mebptt_conv_desc* desc, const void* x, const void*
   Places px, py;
   ConvPlan p;
   if (!conv_check(desc, px, py) || !x || !w || !y) return MEBPTT_ERR_ARG;
-  if (!conv_plan(desc, p)) return MEBPTT_ERR_UNSUPPORTED;
+  if (!conv_plan(desc, false, p)) return MEBPTT_ERR_UNSUPPORTED;
   ConvArgs a = {};
   a.x = x; a.w = w; a.bias = bias; a.s_in = s_in; a.lengths = lengths; a.y = y; a.s_out = s_out;
   return conv_run(desc, p, px, py, a, false, (cudaStream_t)stream);
@@ -365,7 +377,7 @@ int mebptt_conv_forward(const mebptt_conv_desc* desc, const void* x, const void*
 size_t mebptt_conv_workspace_bytes(const mebptt_conv_desc* desc) {
   Places px, py;
   ConvPlan p;
-  if (!conv_check(desc, px, py) || !conv_plan(desc, p)) return 0;
+  if (!conv_check(desc, px, py) || !conv_plan(desc, true, p)) return 0;
   return (size_t)p.blocks * (desc->width + 1) * desc->channels * sizeof(float);
 }
 
@@ -375,7 +387,7 @@ int mebptt_conv_backward(const mebptt_conv_desc* desc, const void* x, const void
   Places px, py;
   ConvPlan p;
   if (!conv_check(desc, px, py) || !x || !w || !dy || !dx || !dw || !natural(dw, 4) || !natural(dbias, 4)) return MEBPTT_ERR_ARG;
-  if (!conv_plan(desc, p)) return MEBPTT_ERR_UNSUPPORTED;
+  if (!conv_plan(desc, true, p)) return MEBPTT_ERR_UNSUPPORTED;
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < mebptt_conv_workspace_bytes(desc))
     return MEBPTT_ERR_WORKSPACE;
   ConvArgs a = {};

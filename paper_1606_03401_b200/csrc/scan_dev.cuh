@@ -11,39 +11,6 @@
 namespace mebptt {
 namespace seq {
 
-// Two floats in a register pair: one instruction works on both (the scan is bound by instruction issue and by the special
-// function unit, not by memory).
-using pair = unsigned long long;
-__device__ __forceinline__ pair pack2(float lo, float hi) {
-  pair r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
-  return r;
-}
-__device__ __forceinline__ float2 unpack2(pair v) {
-  float2 f;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(v));
-  return f;
-}
-__device__ __forceinline__ pair mul2(pair a, pair b) {
-  pair r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ pair add2(pair a, pair b) {
-  pair r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ pair fma2(pair a, pair b, pair c) {
-  pair r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
-__device__ __forceinline__ pair both(float v) { return pack2(v, v); }
-__device__ __forceinline__ float sum2(pair v) {
-  const float2 f = unpack2(v);
-  return f.x + f.y;
-}
 // exp(dt A) of two states, A in units of log 2
 __device__ __forceinline__ pair decay2(pair dt, pair A) {
   const float2 x = unpack2(mul2(dt, A));

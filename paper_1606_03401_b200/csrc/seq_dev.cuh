@@ -27,7 +27,7 @@ __device__ __forceinline__ float from_f<float>(float v) { return v; }
 template <>
 __device__ __forceinline__ bf16 from_f<bf16>(float v) { return __float2bfloat16(v); }   // to nearest: half a step of the type
 
-// N consecutive elements (8, 16 or 32 bytes of them) as they lie in memory.
+// N consecutive elements (4 to 32 bytes of them) as they lie in memory.
 template <class T, int N>
 struct Raw {
   static constexpr int W = N * (int)sizeof(T) / 4;   // 32-bit words
@@ -39,7 +39,9 @@ template <int N, class T>
 __device__ __forceinline__ Raw<T, N> load_raw(const T* p, int n, bool whole) {
   Raw<T, N> r;
   if (whole) {
-    if constexpr (sizeof r == 8) {
+    if constexpr (sizeof r == 4) {
+      r.w[0] = *reinterpret_cast<const uint32_t*>(p);
+    } else if constexpr (sizeof r == 8) {
       const uint2 v = *reinterpret_cast<const uint2*>(p);
       r.w[0] = v.x; r.w[1] = v.y;
     } else {
@@ -85,7 +87,9 @@ __device__ __forceinline__ void store_n(T* p, const float (&f)[N], int n, bool w
     for (int i = 0; i < N; ++i) e[i] = from_f<T>(f[i]);
     Raw<T, N> r;
     memcpy(&r, e, sizeof r);
-    if constexpr (sizeof r == 8) {
+    if constexpr (sizeof r == 4) {
+      *reinterpret_cast<uint32_t*>(p) = r.w[0];
+    } else if constexpr (sizeof r == 8) {
       *reinterpret_cast<uint2*>(p) = make_uint2(r.w[0], r.w[1]);
     } else {
 #pragma unroll
@@ -128,6 +132,65 @@ __device__ __forceinline__ float softplus(float x) {
   p = fmaf(p, q, 1.f / 3.f);
   p = fmaf(p, q, 1.f);
   return fmaf(2.f * t, p, fmaxf(x, 0.f));   // a NaN comes through t
+}
+
+// Two floats in a register pair: one instruction works on both.
+using pair = unsigned long long;
+__device__ __forceinline__ pair pack2(float lo, float hi) {
+  pair r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ float2 unpack2(pair v) {
+  float2 f;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(v));
+  return f;
+}
+__device__ __forceinline__ pair mul2(pair a, pair b) {
+  pair r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ pair add2(pair a, pair b) {
+  pair r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ pair fma2(pair a, pair b, pair c) {
+  pair r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ pair both(float v) { return pack2(v, v); }
+__device__ __forceinline__ float sum2(pair v) {
+  const float2 f = unpack2(v);
+  return f.x + f.y;
+}
+__device__ __forceinline__ pair sigmoid2(pair x) {
+  const float2 e = unpack2(mul2(x, both(-kLog2e)));
+  const float2 d = unpack2(add2(pack2(ex2(e.x), ex2(e.y)), both(1.f)));
+  return pack2(rcp(d.x), rcp(d.y));
+}
+// pairs of N elements as they lie in memory
+template <int N>
+__device__ __forceinline__ void unpack_pairs(const Raw<bf16, N>& r, pair (&f)[N / 2]) {
+#pragma unroll
+  for (int i = 0; i < N / 2; ++i) f[i] = pack2(__uint_as_float(r.w[i] << 16), __uint_as_float(r.w[i] & 0xffff0000u));
+}
+template <int N>
+__device__ __forceinline__ void unpack_pairs(const Raw<float, N>& r, pair (&f)[N / 2]) {
+#pragma unroll
+  for (int i = 0; i < N / 2; ++i) f[i] = pack2(__uint_as_float(r.w[2 * i]), __uint_as_float(r.w[2 * i + 1]));
+}
+template <int N, class T>
+__device__ __forceinline__ void store_pairs(T* p, const pair (&f)[N / 2], int n, bool whole) {
+  float g[N];
+#pragma unroll
+  for (int i = 0; i < N / 2; ++i) {
+    const float2 v = unpack2(f[i]);
+    g[2 * i] = v.x; g[2 * i + 1] = v.y;
+  }
+  store_n<N>(p, g, n, whole);
 }
 
 __device__ __forceinline__ int row_steps(const int32_t* lengths, int b, int64_t t) {
