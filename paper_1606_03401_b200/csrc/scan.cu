@@ -44,11 +44,11 @@ bool check(const mebptt_scan_desc* d, ScanArgs& a, Cut& c) {
   a.batch = d->batch; a.channels = d->channels; a.states = d->states; a.groups = d->groups; a.gchannels = d->channels / d->groups;
   a.t = (int)d->t; a.spacing = d->spacing; a.softplus = d->flags & MEBPTT_SCAN_SOFTPLUS;
   const int lanes = scan_lanes(d->states), chf = scan_fwd_channels(lanes), chb = scan_bwd_channels(lanes);
-  c.np = 4 * lanes;
+  c.np = 8 * lanes;
   c.blocks_f = (a.gchannels + chf - 1) / chf;
   c.blocks_b = (a.gchannels + chb - 1) / chb;
   cut(d->t, (int64_t)d->groups * c.blocks_f * d->batch, SMS * 4, c.segment_f, c.segments_f);
-  cut(d->t, (int64_t)d->groups * c.blocks_b * d->batch, SMS * 2, c.segment_b, c.segments_b);
+  cut(d->t, (int64_t)d->groups * c.blocks_b * d->batch, SMS * 3, c.segment_b, c.segments_b);
   return true;
 }
 // What a grid can count.

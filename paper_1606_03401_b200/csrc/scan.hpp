@@ -18,8 +18,8 @@ struct ScanArgs {
   const float* s_in; const float* ds_out; const int32_t* lengths;
   void* y; float* s_out; float* kept;
   void* du; void* ddelta; void* dz; float* ds_in;
-  // workspace: states (adjoints) at the ends of segments, [segments + 1][batch][D][4 lanes], and the sums of dt within them;
-  // backward: sums over a block's channels [blocks][t][batch][groups][2][4 lanes], and over the steps of a segment
+  // workspace: states (adjoints) at the ends of segments, [segments + 1][batch][D][8 lanes], and the sums of dt within them;
+  // backward: sums over a block's channels [blocks][t][batch][groups][2][8 lanes], and over the steps of a segment
   float* ends; float* dts;
   float* part_bc; float* part_a; float* part_d; float* part_b;
   Places pu, pd, pz, pb, pc, py;
@@ -30,8 +30,8 @@ struct ScanArgs {
   int vec_d, vec_s;                                  // whole groups of 8 channels, of 4 states, load as one
 };
 
-// Lanes that share a channel, four states each.
-inline int scan_lanes(int states) { return states <= 4 ? 1 : states <= 8 ? 2 : states <= 16 ? 4 : states <= 32 ? 8 : 16; }
+// Lanes that share a channel, eight states each.
+inline int scan_lanes(int states) { return states <= 8 ? 1 : states <= 16 ? 2 : states <= 32 ? 4 : 8; }
 
 }  // namespace seq
 }  // namespace mebptt

@@ -11,53 +11,76 @@
 namespace mebptt {
 namespace seq {
 
-// exp(dt A) of two states, A in units of log 2
+// exp(dt A) of two states, A in units of log 2.  The instruction's results are 2e-8 too small on average (measured between -0.5
+// and -0.002, where a state lasts for hundreds of steps and the error of its decay is raised to their power); the constant takes
+// that back, and leaves exp(0) = 1.
+constexpr float kDecayUp = 2.2e-8f;
 __device__ __forceinline__ pair decay2(pair dt, pair A) {
-  const float2 x = unpack2(mul2(dt, A));
+  const float2 x = unpack2(fma2(dt, A, both(kDecayUp)));
   return pack2(ex2(x.x), ex2(x.y));
 }
 
-// Four states of a lane.
-struct Four {
-  pair a, b;
-};
-__device__ __forceinline__ Four lds4(const float* p) {
-  const ulonglong2 v = *reinterpret_cast<const ulonglong2*>(p);
-  return Four{v.x, v.y};
+constexpr int PER_LANE = 8;     // states of a lane, as four pairs
+
+// Pair i of a lane's states lies here, from the first of them on.  `turn` exchanges pairs: bit 1 the halves of four states, bit 0 the
+// pairs of a half (lanes with other channels hold their states in another order, see sum_channels).
+__device__ __forceinline__ int pair_at(int i, int turn) { return 2 * (i ^ turn); }
+
+__device__ __forceinline__ pair load_pair(const float* row, int n0, int states, bool vec) {
+  if (vec && n0 + 2 <= states) return *reinterpret_cast<const pair*>(row + n0);
+  return pack2(n0 < states ? row[n0] : 0.f, n0 + 1 < states ? row[n0 + 1] : 0.f);
 }
-__device__ __forceinline__ void st4(float* p, const Four& f) {
-  *reinterpret_cast<ulonglong2*>(p) = make_ulonglong2(f.a, f.b);
-}
-// Four of `states` values of a row (channel) from n0 on, zeros past the last.
-__device__ __forceinline__ Four load_states(const float* row, int n0, int states, bool vec) {
-  if (vec && n0 + 4 <= states) return lds4(row + n0);
-  float f[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) f[i] = n0 + i < states ? row[n0 + i] : 0.f;
-  return Four{pack2(f[0], f[1]), pack2(f[2], f[3])};
-}
-__device__ __forceinline__ void store_states(float* row, int n0, int states, bool vec, const Four& v) {
-  if (vec && n0 + 4 <= states) {
-    st4(row + n0, v);
+__device__ __forceinline__ void store_pair(float* row, int n0, int states, bool vec, pair v) {
+  if (vec && n0 + 2 <= states) {
+    *reinterpret_cast<pair*>(row + n0) = v;
     return;
   }
-  const float2 x = unpack2(v.a), y = unpack2(v.b);
-  const float f[4] = {x.x, x.y, y.x, y.y};
+  const float2 f = unpack2(v);
+  if (n0 < states) row[n0] = f.x;
+  if (n0 + 1 < states) row[n0 + 1] = f.y;
+}
+// A lane's states out of a row of `states` values (zeros past the last), and back: in their own order, and in a lane's.
+__device__ __forceinline__ void load_states(const float* row, int l, int states, bool vec, pair (&s)[4]) {
+  if (vec && PER_LANE * (l + 1) <= states) {
+    const ulonglong2* const p = reinterpret_cast<const ulonglong2*>(row + PER_LANE * l);
+    const ulonglong2 a = p[0], b = p[1];
+    s[0] = a.x; s[1] = a.y; s[2] = b.x; s[3] = b.y;
+    return;
+  }
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (n0 + i < states) row[n0 + i] = f[i];
+  for (int i = 0; i < 4; ++i) s[i] = load_pair(row, PER_LANE * l + 2 * i, states, vec);
+}
+__device__ __forceinline__ void store_states(float* row, int l, int states, bool vec, const pair (&s)[4]) {
+  if (vec && PER_LANE * (l + 1) <= states) {
+    ulonglong2* const p = reinterpret_cast<ulonglong2*>(row + PER_LANE * l);
+    p[0] = make_ulonglong2(s[0], s[1]);
+    p[1] = make_ulonglong2(s[2], s[3]);
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) store_pair(row, PER_LANE * l + 2 * i, states, vec, s[i]);
+}
+__device__ __forceinline__ void load_states(const float* row, int l, int turn, int states, bool vec, pair (&s)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) s[i] = load_pair(row, PER_LANE * l + pair_at(i, turn), states, vec);
+}
+__device__ __forceinline__ void store_states(float* row, int l, int turn, int states, bool vec, const pair (&s)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) store_pair(row, PER_LANE * l + pair_at(i, turn), states, vec, s[i]);
 }
 
-// Where (channel, step) of a tile lies in shared memory: steps of a channel together, so that a lane loads four at once; groups of
-// four steps are exchanged by channel group, so that neither the walk along steps nor that along channels meets a bank twice.
-template <int STEPS>
-__device__ __forceinline__ int at(int c, int step) {
-  return c * (STEPS + 4) + ((((step >> 2) ^ (2 * (c >> 3))) & (STEPS / 4 - 1)) << 2 | (step & 3));
-}
-template <int STEPS>
-__device__ __forceinline__ float4 four_steps(const float* tile, int c, int step) {
-  return *reinterpret_cast<const float4*>(tile + at<STEPS>(c, step));
-}
+// Where (channel, step) of a tile lies in shared memory: steps of a channel together, so that a lane loads four at once, and groups of
+// eight channels shifted against one another, so that neither the walk along steps nor that along channels meets a bank twice.
+template <int STEPS, int CH>
+struct Tile {
+  static constexpr int SKEW = 256 / CH < 4 ? 4 : 256 / CH;
+  static constexpr int FLOATS = CH * (STEPS + 4) + CH / 8 * SKEW;
+  static __device__ __forceinline__ int at(int c, int step) { return c * (STEPS + 4) + (c >> 3) * SKEW + step; }
+  static __device__ __forceinline__ void four(const float* tile, int c, int step, float (&v)[4]) {
+    const float4 f = *reinterpret_cast<const float4*>(tile + at(c, step));
+    v[0] = f.x; v[1] = f.y; v[2] = f.z; v[3] = f.w;
+  }
+};
 
 // Sums of v[0..3] (four steps) over the LANES lanes of a channel.  With four lanes or more, lane l gets step l % 4 in v[0]; with two,
 // lane l gets steps 2 l and 2 l + 1; with one, all four.
@@ -83,6 +106,14 @@ template <int LANES>
 constexpr int steps_of_lane = LANES >= 4 ? 1 : 4 / LANES;
 template <int LANES>
 __device__ __forceinline__ int first_step(int l) { return LANES >= 4 ? (l & 3) : l * steps_of_lane<LANES>; }
+// what sum_lanes left to a lane, to the places of its steps
+template <int LANES>
+__device__ __forceinline__ void put_steps(float* at, int l, const float (&v)[4]) {
+  float* const p = at + first_step<LANES>(l);
+  if constexpr (LANES == 1) *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+  else if constexpr (LANES == 2) *reinterpret_cast<float2*>(p) = make_float2(v[0], v[1]);
+  else *p = v[0];
+}
 
 __device__ __forceinline__ float step_size(float pre, int soft) { return soft ? softplus(pre) : pre; }
 
@@ -90,6 +121,15 @@ __device__ __forceinline__ float step_size(float pre, int soft) { return soft ? 
 __device__ __forceinline__ pair carry2(pair A, float dts, pair v, pair end) {
   const float2 p = unpack2(decay2(both(dts), A)), x = unpack2(v), e = unpack2(end);
   return pack2(x.x == 0.f ? e.x : fmaf(p.x, x.x, e.x), x.y == 0.f ? e.y : fmaf(p.y, x.y, e.y));
+}
+// sum over a lane's states of x y
+__device__ __forceinline__ float dot(const pair (&x)[4], const pair (&y)[4]) {
+  return sum2(add2(fma2(x[0], y[0], mul2(x[1], y[1])), fma2(x[2], y[2], mul2(x[3], y[3]))));
+}
+// a lane's eight values of a row in shared memory
+__device__ __forceinline__ void lds8(const float* p, pair (&v)[4]) {
+  const ulonglong2 a = *reinterpret_cast<const ulonglong2*>(p), b = *reinterpret_cast<const ulonglong2*>(p + 4);
+  v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y;
 }
 
 }  // namespace seq

@@ -3,7 +3,7 @@
 // Every state decays by a factor of its own, so there is no matrix product in it: a step of a channel takes N exponentials and some
 // 4 N multiply-adds on 8 bytes, and the special function unit (16 exponentials a clock and SM) bounds it, at three times what
 // the memory would allow for N = 16.  A block owns 128 / LANES channels of one row and walks its steps in tiles; LANES lanes
-// share a channel, four states each in registers.  Per tile: the elementwise part (dt, dt u) eight channels of a step to a
+// share a channel, eight states each in registers, two to an instruction.  Per tile: the elementwise part (dt, dt u) eight channels of a step to a
 // thread, with 16-byte loads issued a tile ahead; the scan out of shared memory; the gate, again elementwise.
 //
 // Few rows and channels leave SMs without work, so long sequences are then cut into segments: a first kernel finds the state
@@ -32,19 +32,22 @@ template <int LANES>
 struct Shape {
   static constexpr int CH = NT / LANES;                                                      // channels of a block
   static constexpr int STEPS = LANES == 1 ? 8 : LANES == 2 ? 16 : 32;                        // of a tile: no more than a group of channels a thread
-  static constexpr int NP = 4 * LANES;                                                       // states, with those that pad
-  static constexpr int PB = STEPS * 2 * LANES <= NT ? 1 : STEPS * 2 * LANES / NT;            // quarters of B and C rows a thread loads
-  static constexpr int FLOATS = 2 * CH * (STEPS + 4) + STEPS * 2 * NP;
+  static constexpr int NP = PER_LANE * LANES;                                                // states, with those that pad
+  static constexpr int QUARTERS = STEPS * 2 * NP / 4;                                        // of the rows of B and C, four states each
+  static constexpr int PB = QUARTERS <= NT ? 1 : QUARTERS / NT;                              // of a thread
+  using At = Tile<STEPS, CH>;
+  static constexpr int FLOATS = 2 * At::FLOATS + STEPS * 2 * NP;
 };
 
 template <class T, int LANES, int PASS>
 __global__ void __launch_bounds__(NT) scan_fwd(const ScanArgs a) {
   using S = Shape<LANES>;
   constexpr int CH = S::CH, STEPS = S::STEPS, NP = S::NP, PB = S::PB;
+  using At = typename S::At;
   __shared__ __align__(16) float sm[S::FLOATS];
   float* const s_dt = sm;                              // [CH][STEPS]: dt, later the sums over states; ADJOINTS: dt
-  float* const s_x = sm + CH * (STEPS + 4);            // dt u; ADJOINTS: dy times the gate
-  float* const s_bc = sm + 2 * CH * (STEPS + 4);       // [STEPS][B, C][NP]
+  float* const s_x = sm + At::FLOATS;                  // dt u; ADJOINTS: dy times the gate
+  float* const s_bc = sm + 2 * At::FLOATS;       // [STEPS][B, C][NP]
 
   const int tid = threadIdx.x, b = blockIdx.y, seg = blockIdx.z + (PASS == ADJOINTS);   // segment 0 hands its adjoint to none
   const int g = blockIdx.x / a.blocks, base = (blockIdx.x % a.blocks) * CH;     // first channel, within the group
@@ -66,34 +69,37 @@ __global__ void __launch_bounds__(NT) scan_fwd(const ScanArgs a) {
   const T* const Bm = (const T*)a.B + (int64_t)b * a.pb.row + g * a.states;
   const T* const Cm = (const T*)a.C + (int64_t)b * a.pc.row + g * a.states;
 
-  // scan: a channel and four of its states
+  // scan: a channel and eight of its states
   const int c = tid / LANES, l = tid % LANES;
   const bool mine = c < live;
   const int d = d0 + c;
-  Four A = {0, 0}, s = {0, 0};
+  pair A[4] = {}, s[4] = {};
   if (mine) {
-    A = load_states(a.A + (int64_t)d * a.states, 4 * l, a.states, a.vec_s);
-    const pair k = both(kLog2e);
-    A.a = mul2(A.a, k); A.b = mul2(A.b, k);
+    load_states(a.A + (int64_t)d * a.states, l, a.states, a.vec_s, A);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) A[i] = mul2(A[i], both(kLog2e));
   }
-  const int64_t place = ((int64_t)b * a.channels + d) * NP + 4 * l;             // of this lane's states in a layer of `ends`
+  const int64_t place = ((int64_t)b * a.channels + d) * NP;                     // of this channel's states in a layer of `ends`
   const int64_t layer = (int64_t)a.batch * a.channels * NP;
+  const int64_t row = ((int64_t)b * a.channels + d) * a.states;
   if (PASS == OUTPUTS && a.segments > 1) {
     if (mine) {
-      s = lds4(a.ends + place);
+      load_states(a.ends + place, l, NP, true, s);
       for (int j = 0; j < seg; ++j) {
-        const Four e = lds4(a.ends + (j + 1) * layer + place);
+        pair e[4];
+        load_states(a.ends + (j + 1) * layer + place, l, NP, true, e);
         const float dts = a.dts[((int64_t)j * a.batch + b) * a.channels + d];
-        s.a = carry2(A.a, dts, s.a, e.a);
-        s.b = carry2(A.b, dts, s.b, e.b);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[i] = carry2(A[i], dts, s[i], e[i]);
       }
     }
   } else if (PASS == OUTPUTS || (PASS == ENDS && seg == 0)) {
-    if (mine && a.s_in) s = load_states(a.s_in + ((int64_t)b * a.channels + d) * a.states, 4 * l, a.states, a.vec_s);
+    if (mine && a.s_in) load_states(a.s_in + row, l, a.states, a.vec_s, s);
     if (PASS == ENDS) {
       // the second kernel has the first states from here, as s_out may be where s_in lies
-      if (mine) st4(a.ends + place, s);
-      s = Four{0, 0};
+      if (mine) store_states(a.ends + place, l, NP, true, s);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[i] = 0;
     }
   }
 
@@ -116,8 +122,8 @@ __global__ void __launch_bounds__(NT) scan_fwd(const ScanArgs a) {
     if (PASS != ENDS && a.z) rz = in ? load_raw<8>(z + (int64_t)k * a.pz.step, en, whole) : raw_zeros<T, 8>();
 #pragma unroll
     for (int i = 0; i < PB; ++i) {
-      const int q = tid + i * NT, n4 = (q % LANES) * 4, which = (q / LANES) & 1, step = k0 + q / (2 * LANES);
-      const bool used = q < STEPS * 2 * LANES && step < n && step < last && n4 < a.states && (PASS == OUTPUTS || which == (PASS == ADJOINTS));
+      const int q = tid + i * NT, n4 = (q % (NP / 4)) * 4, which = (q / (NP / 4)) & 1, step = k0 + q / (NP / 2);
+      const bool used = q < S::QUARTERS && step < n && step < last && n4 < a.states && (PASS == OUTPUTS || which == (PASS == ADJOINTS));
       const T* p = which ? Cm + (int64_t)step * a.pc.step : Bm + (int64_t)step * a.pb.step;
       rbc[i] = used ? load_raw<4>(p + n4, a.states - n4, a.vec_s && n4 + 4 <= a.states) : raw_zeros<T, 4>();
     }
@@ -138,19 +144,19 @@ __global__ void __launch_bounds__(NT) scan_fwd(const ScanArgs a) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const float dt = in ? step_size(pre[j] + fbias[j], a.softplus) : 0.f;
-        s_dt[at<STEPS>(ec + j, es)] = dt;
-        if (PASS != ADJOINTS) s_x[at<STEPS>(ec + j, es)] = in ? dt * fu[j] : 0.f;
+        s_dt[At::at(ec + j, es)] = dt;
+        if (PASS != ADJOINTS) s_x[At::at(ec + j, es)] = in ? dt * fu[j] : 0.f;
       }
       if (PASS != ENDS && a.z) unpack<8>(rz, fz);
       if (PASS == ADJOINTS) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) s_x[at<STEPS>(ec + j, es)] = a.z ? fu[j] * fz[j] * sigmoid(fz[j]) : fu[j];
+        for (int j = 0; j < 8; ++j) s_x[At::at(ec + j, es)] = a.z ? fu[j] * fz[j] * sigmoid(fz[j]) : fu[j];
       }
     }
 #pragma unroll
     for (int q = 0; q < PB; ++q) {
       const int e = tid + q * NT;
-      if (e < STEPS * 2 * LANES) {
+      if (e < S::QUARTERS) {
         float f[4];
         unpack<4>(rbc[q], f);
         *reinterpret_cast<float4*>(s_bc + e * 4) = make_float4(f[0], f[1], f[2], f[3]);
@@ -161,34 +167,32 @@ __global__ void __launch_bounds__(NT) scan_fwd(const ScanArgs a) {
     const int steps = min(STEPS, min(n, last) - k0);
     for (int jj = 0; jj < steps; jj += 4) {
       const int j0 = PASS == ADJOINTS ? (steps - 1) / 4 * 4 - jj : jj;
-      const float4 dt4 = four_steps<STEPS>(s_dt, c, j0), x4 = four_steps<STEPS>(s_x, c, j0);
-      const float dt[4] = {dt4.x, dt4.y, dt4.z, dt4.w}, x[4] = {x4.x, x4.y, x4.z, x4.w};
+      float dt[4], x[4], part[4];
+      At::four(s_dt, c, j0, dt);
+      At::four(s_x, c, j0, x);
       if (PASS == OUTPUTS && a.kept && ((k0 + j0) & (a.spacing - 1)) == 0 && mine)
-        st4(a.kept + (int64_t)((k0 + j0) / a.spacing) * layer + place, s);
-      float part[4];
+        store_states(a.kept + (int64_t)((k0 + j0) / a.spacing) * layer + place, l, NP, true, s);
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         const int j = PASS == ADJOINTS ? 3 - q : q;
         const pair dt2 = both(dt[j]), x2 = both(x[j]);
-        const Four in = lds4(s_bc + ((j0 + j) * 2 + (PASS == ADJOINTS)) * NP + 4 * l);
-        const pair ea = decay2(dt2, A.a), eb = decay2(dt2, A.b);
-        if (PASS == ADJOINTS) {
-          s.a = mul2(ea, fma2(x2, in.a, s.a));
-          s.b = mul2(eb, fma2(x2, in.b, s.b));
-        } else {
-          s.a = fma2(ea, s.a, mul2(x2, in.a));
-          s.b = fma2(eb, s.b, mul2(x2, in.b));
+        const float* const bc = s_bc + (j0 + j) * 2 * NP + PER_LANE * l;
+        pair in[4], C[4];
+        lds8(bc + (PASS == ADJOINTS ? NP : 0), in);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const pair e = decay2(dt2, A[i]);
+          s[i] = PASS == ADJOINTS ? mul2(e, fma2(x2, in[i], s[i])) : fma2(e, s[i], mul2(x2, in[i]));
         }
         if (PASS != OUTPUTS) dts += dt[j];
         if (PASS == OUTPUTS) {
-          const Four C = lds4(s_bc + ((j0 + j) * 2 + 1) * NP + 4 * l);
-          part[j] = sum2(fma2(C.a, s.a, mul2(C.b, s.b)));
+          lds8(bc + NP, C);
+          part[j] = dot(C, s);
         }
       }
       if (PASS == OUTPUTS) {
         sum_lanes<LANES>(part, l);
-#pragma unroll
-        for (int q = 0; q < steps_of_lane<LANES>; ++q) s_dt[at<STEPS>(c, j0 + first_step<LANES>(l) + q)] = part[q];
+        put_steps<LANES>(s_dt + At::at(c, j0), l, part);
       }
     }
     __syncthreads();
@@ -197,7 +201,7 @@ __global__ void __launch_bounds__(NT) scan_fwd(const ScanArgs a) {
       float out[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float v = fmaf(fskip[j], fu[j], s_dt[at<STEPS>(ec + j, es)]);
+        const float v = fmaf(fskip[j], fu[j], s_dt[At::at(ec + j, es)]);
         out[j] = !in ? 0.f : a.z ? v * fz[j] * sigmoid(fz[j]) : v;
       }
       store_n<8>(y + (int64_t)(k0 + es) * a.py.step, out, en, whole);
@@ -208,9 +212,9 @@ __global__ void __launch_bounds__(NT) scan_fwd(const ScanArgs a) {
     float zero[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     if (worker)
       for (int k = first + busy * STEPS + es; k < last; k += STEPS) store_n<8>(y + (int64_t)k * a.py.step, zero, en, whole);
-    if (mine && a.s_out && seg == a.segments - 1) store_states(a.s_out + ((int64_t)b * a.channels + d) * a.states, 4 * l, a.states, a.vec_s, s);
+    if (mine && a.s_out && seg == a.segments - 1) store_states(a.s_out + row, l, a.states, a.vec_s, s);
   } else if (mine) {
-    st4(a.ends + (int64_t)(seg + 1) * layer + place, s);
+    store_states(a.ends + (int64_t)(seg + 1) * layer + place, l, NP, true, s);
     if (l == 0) a.dts[((int64_t)seg * a.batch + b) * a.channels + d] = dts;
   }
 }
@@ -219,45 +223,51 @@ __global__ void __launch_bounds__(NT) scan_fwd(const ScanArgs a) {
 constexpr int NT1 = 256;
 template <class T, int LANES>
 __global__ void __launch_bounds__(NT1) scan_token(const ScanArgs a) {
-  constexpr int CH = NT1 / LANES, NP = 4 * LANES;
+  constexpr int CH = NT1 / LANES, NP = PER_LANE * LANES;
   const int b = blockIdx.y, c = threadIdx.x / LANES, l = threadIdx.x % LANES;
   const int64_t d = (int64_t)blockIdx.x * CH + c;
   const bool mine = d < a.channels;
   const int n = row_steps(a.lengths, b, 1);
-  Four A = {0, 0}, s = {0, 0}, B = {0, 0}, C = {0, 0};
+  pair A[4] = {}, s[4] = {}, B[4] = {}, C[4] = {};
   float u = 0.f, pre = 0.f, z = 0.f, skip = 0.f;
+  const int64_t row = ((int64_t)b * a.channels + d) * a.states;
   if (mine) {
-    if (a.s_in) s = load_states(a.s_in + ((int64_t)b * a.channels + d) * a.states, 4 * l, a.states, a.vec_s);
+    if (a.s_in) load_states(a.s_in + row, l, a.states, a.vec_s, s);
     if (n > 0) {
-      A = load_states(a.A + d * a.states, 4 * l, a.states, a.vec_s);
-      const int g = (int)(d / a.gchannels), n4 = 4 * l;
-      float f[4];
-      if (n4 < a.states) {
-        const bool vec = a.vec_s && n4 + 4 <= a.states;
-        unpack<4>(load_raw<4>((const T*)a.B + (int64_t)b * a.pb.row + g * a.states + n4, a.states - n4, vec), f);
-        B = Four{pack2(f[0], f[1]), pack2(f[2], f[3])};
-        unpack<4>(load_raw<4>((const T*)a.C + (int64_t)b * a.pc.row + g * a.states + n4, a.states - n4, vec), f);
-        C = Four{pack2(f[0], f[1]), pack2(f[2], f[3])};
-      }
+      load_states(a.A + d * a.states, l, a.states, a.vec_s, A);
+      const int g = (int)(d / a.gchannels);
+      auto load = [&](const void* base, const Places& p, pair (&v)[4]) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int n4 = PER_LANE * l + 4 * h;
+          if (n4 >= a.states) continue;
+          pair f[2];
+          unpack_pairs<4>(load_raw<4>((const T*)base + (int64_t)b * p.row + g * a.states + n4, a.states - n4, a.vec_s && n4 + 4 <= a.states), f);
+          v[2 * h] = f[0];
+          v[2 * h + 1] = f[1];
+        }
+      };
+      load(a.B, a.pb, B);
+      load(a.C, a.pc, C);
       u = to_f<T>(((const T*)a.u)[(int64_t)b * a.pu.row + d]);
       pre = to_f<T>(((const T*)a.delta)[(int64_t)b * a.pd.row + d]) + (a.bias ? a.bias[d] : 0.f);
       if (a.z) z = to_f<T>(((const T*)a.z)[(int64_t)b * a.pz.row + d]);
       if (a.skip) skip = a.skip[d];
     }
-    if (a.kept) st4(a.kept + ((int64_t)b * a.channels + d) * NP + 4 * l, s);
+    if (a.kept) store_states(a.kept + ((int64_t)b * a.channels + d) * NP, l, NP, true, s);
   }
   float v = 0.f;
   if (n > 0) {
     const float dt = step_size(pre, a.softplus);
-    const pair dt2 = both(dt), x2 = both(dt * u), k = both(kLog2e);
-    s.a = fma2(decay2(dt2, mul2(A.a, k)), s.a, mul2(x2, B.a));
-    s.b = fma2(decay2(dt2, mul2(A.b, k)), s.b, mul2(x2, B.b));
-    v = sum2(fma2(C.a, s.a, mul2(C.b, s.b)));
+    const pair dt2 = both(dt), x2 = both(dt * u);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[i] = fma2(decay2(dt2, mul2(A[i], both(kLog2e))), s[i], mul2(x2, B[i]));
+    v = dot(C, s);
   }
 #pragma unroll
   for (int m = 1; m < LANES; m *= 2) v += __shfl_xor_sync(0xffffffffu, v, m);
   if (!mine) return;
-  if (a.s_out) store_states(a.s_out + ((int64_t)b * a.channels + d) * a.states, 4 * l, a.states, a.vec_s, s);
+  if (a.s_out) store_states(a.s_out + row, l, a.states, a.vec_s, s);
   if (l == 0) {
     v = fmaf(skip, u, v);
     ((T*)a.y)[(int64_t)b * a.py.row + d] = from_f<T>(n > 0 ? (a.z ? v * z * sigmoid(z) : v) : 0.f);
@@ -294,8 +304,7 @@ int scan_fwd_channels(int lanes) { return NT / lanes; }
     case 1: return F<T, 1>(a, s);               \
     case 2: return F<T, 2>(a, s);               \
     case 4: return F<T, 4>(a, s);               \
-    case 8: return F<T, 8>(a, s);               \
-    default: return F<T, 16>(a, s);             \
+    default: return F<T, 8>(a, s);              \
   }
 void scan_forward(const ScanArgs& a, bool half, cudaStream_t s) {
   if (half) { BY_LANES(launch, bf16) }
