@@ -1,10 +1,10 @@
 // Selective state space scan, backward.
 //
-// A block owns 128 / LANES channels of one row and walks a segment's tiles of 32 steps from the last to the first; LANES lanes share
+// A block owns 128 / LANES channels of one row and walks a segment's tiles of 16 steps from the last to the first; LANES lanes share
 // a channel, eight states each, two to an instruction.  States are not kept but every `spacing` steps: eight steps at a time are
 // run forwards from the state before them, with the decays and the states of the eight steps in registers, and then backwards.
-// Where states are kept further apart, a tile first runs forwards once more to have the state before each of its eights (one
-// exponential more for each state and step).
+// Where states are kept further apart, those between are found by running forwards once more.  Every thread fetches the next
+// tile's inputs and states while a tile is worked on (12 warps an SM would not hide them).
 //
 // Sums go three ways.  Over the states of a channel (v, g B, A a s g): the lanes of a channel, four steps at a time, each lane ending
 // with steps of its own.  Over channels (dB, dC): halving exchanges among the lanes of a warp with the same states, then the
@@ -30,19 +30,23 @@ namespace seq {
 
 namespace {
 
-constexpr int EIGHT = 8, NT = 128;
+constexpr int EIGHT = 8, NT = 128, STEPS = 16;     // steps of a tile
 
-template <int LANES>
+template <class T, int LANES>
 struct Shape {
   static constexpr int CH = NT / LANES, NP = PER_LANE * LANES, WARPS = NT / 32;
-  static constexpr int CHUNKS = TILE * CH / 8 / NT > 0 ? TILE * CH / 8 / NT : 1;    // groups of eight channels a thread, in the elementwise part
-  using At = Tile<TILE, CH>;
+  static constexpr int CHUNKS = STEPS * CH / 8 > NT ? STEPS * CH / 8 / NT : 1;      // groups of eight channels a thread, in the elementwise part
+  static constexpr int QUARTERS = STEPS * NP / 2;                                   // of B and C: four states each
+  static constexpr int QB = QUARTERS > NT ? QUARTERS / NT : 1;                      // of a thread
+  using At = Tile<STEPS, CH>;
   static constexpr int ORDERS = 4;                                                  // of B and C
   static constexpr int ROW = ORDERS * NP;                                           // of B or C, of a step
   static constexpr int RED = WARPS * EIGHT * 2 * NP;                                // sums of one eight, by warp
-  // planes of the tile, B and C, sums, and the channels' bias and skip; states before the eights of a tile if they are not kept
-  static constexpr int FLOATS = 4 * At::FLOATS + TILE * 2 * ROW + 2 * RED + 2 * CH + NT * PER_LANE;
-  static constexpr int STARTS = 3 * NT * PER_LANE;
+  // What a thread fetches for a tile, in 16-byte pieces: u, delta, dy, z; B and C; two states.  Each thread reads what it fetched itself.
+  static constexpr int ARRAY = CHUNKS * (int)sizeof(T) / 2, BC = QB * (int)sizeof(T) / 4 > 0 ? QB * (int)sizeof(T) / 4 : 1;
+  static constexpr int PIECES = 4 * ARRAY + BC + 4;
+  // planes of the tile, B and C, sums of an eight and of tiles, the channels' bias and skip, what is fetched (twice)
+  static constexpr int FLOATS = 4 * At::FLOATS + STEPS * 2 * ROW + RED + NT * PER_LANE + 2 * CH + 2 * PIECES * NT * 4;
 };
 
 // Sums of dB and dC (eight values each) over the 32 / LANES lanes with the same states.  Lanes halve the values among them as long as
@@ -93,29 +97,36 @@ __device__ __forceinline__ void load_turned(const float* row, int l, int turn, i
   for (int i = 0; i < 4; ++i) s[i] = load_pair(row, PER_LANE * l + pair_at(i, turn), states, vec);
 }
 
+__device__ __forceinline__ void async16(void* dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src) : "memory");
+}
+__device__ __forceinline__ void async8(void* dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src) : "memory");
+}
+
 template <class T, int LANES, bool GATE>
 __global__ void __launch_bounds__(NT, 3) scan_bwd(const ScanArgs a) {
-  using S = Shape<LANES>;
+  using S = Shape<T, LANES>;
   using At = typename S::At;
-  constexpr int CH = S::CH, NP = S::NP, WARPS = S::WARPS, CHUNKS = S::CHUNKS;
+  constexpr int CH = S::CH, NP = S::NP, WARPS = S::WARPS, CHUNKS = S::CHUNKS, QB = S::QB;
   extern __shared__ __align__(16) float sm[];
-  float* const s_dt = sm;                         // dt
+  uint4* const s_raw = reinterpret_cast<uint4*>(sm);                                // [2][PIECES][NT]
+  float* const s_dt = sm + 2 * S::PIECES * NT * 4;   // dt
   float* const s_x = s_dt + At::FLOATS;           // dt u, then the sums over states of g B, then dv u
   float* const s_dv = s_x + At::FLOATS;           // dv, then of A a s g, then ddelta
   float* const s_v = s_dv + At::FLOATS;           // of C s
-  float* const s_bc = s_v + At::FLOATS;           // [TILE][B, C][two halves of a lane's states][orders][LANES][4]
-  float* const s_red = s_bc + TILE * 2 * S::ROW;  // [2][WARPS][EIGHT][2 NP]
-  float* const s_dA = s_red + 2 * S::RED;         // [NT][8]: sums of the tiles so far
+  float* const s_bc = s_v + At::FLOATS;           // [STEPS][B, C][two halves of a lane's states][orders][LANES][4]
+  float* const s_red = s_bc + STEPS * 2 * S::ROW; // [WARPS][EIGHT][2 NP]
+  float* const s_dA = s_red + S::RED;             // [NT][8]: sums of the tiles so far
   float* const s_bias = s_dA + NT * PER_LANE;     // [CH]
   float* const s_skip = s_bias + CH;              // [CH]
-  float* const s_start = s_skip + CH;             // [3][NT][8]: states before the eights of a tile but the first
 
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, b = blockIdx.y, seg = blockIdx.z;
   const int g = blockIdx.x / a.blocks, block = blockIdx.x % a.blocks, base = block * CH;
   const int d0 = g * a.gchannels + base;
   const int live = min(CH, a.gchannels - base);
   const int n = row_steps(a.lengths, b, a.t);
-  const int first = seg * a.segment, last = min(first + a.segment, a.t);
+  const int first = seg * a.segment, last = min(first + a.segment, a.t), stop = min(n, last);
 
   const T* const Bm = (const T*)a.B + (int64_t)b * a.pb.row + g * a.states;
   const T* const Cm = (const T*)a.C + (int64_t)b * a.pc.row + g * a.states;
@@ -151,23 +162,155 @@ __global__ void __launch_bounds__(NT, 3) scan_bwd(const ScanArgs a) {
   // eight channels of a step, in the elementwise parts
   struct Chunk {
     int ec, es, en;
-    bool in, whole;
+    bool here, whole;
   };
-  auto chunk = [&](int p, int k0) {
+  auto chunk = [&](int p) {
     const int q = tid + p * NT;
     Chunk h;
     h.ec = (q % (CH / 8)) * 8;
     h.es = q / (CH / 8);
     h.en = min(8, live - h.ec);
-    h.in = h.es < TILE && h.en > 0 && k0 + h.es < min(n, last);
+    h.here = h.es < STEPS && h.en > 0;
     h.whole = a.vec_d && h.en == 8;
     return h;
   };
-  auto read = [&](const void* x, const Places& p, const Chunk& h, int k0) {
-    return h.in ? load_raw<8>((const T*)x + (int64_t)(k0 + h.es) * p.step + (int64_t)b * p.row + d0 + h.ec, h.en, h.whole) : raw_zeros<T, 8>();
+  // Asks for the tile at k0: into the thread's own pieces of stage st.  Where groups do not load as one they come by plain loads.
+  auto fetch = [&](int k0, int st) {
+    uint4* const raw = s_raw + st * S::PIECES * NT + tid;
+    auto array = [&](const void* x, const Places& p, int which) {
+#pragma unroll
+      for (int q = 0; q < CHUNKS; ++q) {
+        const Chunk h = chunk(q);
+        if (!h.here || k0 + h.es >= stop) continue;
+        const T* const from = (const T*)x + (int64_t)(k0 + h.es) * p.step + (int64_t)b * p.row + d0 + h.ec;
+        uint4* const to = raw + (which * S::ARRAY + q * (int)sizeof(T) / 2) * NT;
+        if (h.whole) {
+#pragma unroll
+          for (int i = 0; i < (int)sizeof(T) / 2; ++i) async16(to + i * NT, reinterpret_cast<const uint4*>(from) + i);
+        } else {
+          const Raw<T, 8> r = load_raw<8>(from, h.en, false);
+#pragma unroll
+          for (int i = 0; i < (int)sizeof(T) / 2; ++i) to[i * NT] = make_uint4(r.w[4 * i], r.w[4 * i + 1], r.w[4 * i + 2], r.w[4 * i + 3]);
+        }
+      }
+    };
+    array(a.u, a.pu, 0);
+    array(a.delta, a.pd, 1);
+    array(a.dy, a.py, 2);
+    if (GATE) array(a.z, a.pz, 3);
+    uint8_t* const bc = reinterpret_cast<uint8_t*>(raw - tid + 4 * S::ARRAY * NT);
+#pragma unroll
+    for (int i = 0; i < QB; ++i) {
+      const int q = tid + i * NT, n4 = (q % (NP / 4)) * 4, which = (q / (NP / 4)) & 1, k = k0 + q / (NP / 2);
+      if (q >= S::QUARTERS || k >= stop || n4 >= a.states) continue;
+      const T* const from = (which ? Cm + (int64_t)k * a.pc.step : Bm + (int64_t)k * a.pb.step) + n4;
+      void* const to = bc + (size_t)q * 4 * sizeof(T);
+      if (a.vec_s && n4 + 4 <= a.states) {
+        if constexpr (sizeof(T) == 2) async8(to, from);
+        else async16(to, from);
+      } else {
+        const Raw<T, 4> r = load_raw<4>(from, a.states - n4, false);
+        memcpy(to, &r, sizeof r);
+      }
+    }
+    if (mine) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int k = k0 + e * EIGHT;
+        if (k >= stop || (k & (a.spacing - 1))) continue;
+        const uint4* const from = reinterpret_cast<const uint4*>(a.kept + (int64_t)(k / a.spacing) * layer + place + PER_LANE * l);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) async16(raw + (4 * S::ARRAY + S::BC + 2 * e + i) * NT, from + i);
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  auto write = [&](void* x, const Places& p, const Chunk& h, int k0, const float (&f)[8]) {
-    store_n<8>((T*)x + (int64_t)(k0 + h.es) * p.step + (int64_t)b * p.row + d0 + h.ec, f, h.en, h.whole);
+  auto raw_chunk = [&](int st, int which, int q) {
+    const uint4* const p = s_raw + st * S::PIECES * NT + tid + (which * S::ARRAY + q * (int)sizeof(T) / 2) * NT;
+    Raw<T, 8> r;
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+      const uint4 v = p[i * NT];
+      r.w[4 * i] = v.x; r.w[4 * i + 1] = v.y; r.w[4 * i + 2] = v.z; r.w[4 * i + 3] = v.w;
+    }
+    return r;
+  };
+  auto kept_state = [&](int st, int e, pair (&s)[4]) {       // pairs 2 i and 2 i + 1 lie in piece i
+    const pair* const p = reinterpret_cast<const pair*>(s_raw + st * S::PIECES * NT + tid + (4 * S::ARRAY + S::BC + 2 * e) * NT);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int at = i ^ turn;
+      s[i] = mine ? p[(at >> 1) * 2 * NT + (at & 1)] : 0;
+    }
+  };
+  auto write = [&](void* x, const Places& p, const Chunk& h, int k0, const pair (&f)[4]) {
+    store_pairs<8>((T*)x + (int64_t)(k0 + h.es) * p.step + (int64_t)b * p.row + d0 + h.ec, f, h.en, h.whole);
+  };
+  // eight values of a plane at one step
+  auto plane = [&](const float* s, const Chunk& h, pair (&f)[4]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) f[j] = pack2(s[At::at(h.ec + 2 * j, h.es)], s[At::at(h.ec + 2 * j + 1, h.es)]);
+  };
+  auto to_plane = [&](float* s, const Chunk& h, const pair (&f)[4]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float2 v = unpack2(f[j]);
+      s[At::at(h.ec + 2 * j, h.es)] = v.x;
+      s[At::at(h.ec + 2 * j + 1, h.es)] = v.y;
+    }
+  };
+  auto channel_values = [&](const float* s, const Chunk& h, pair (&f)[4]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) f[j] = *reinterpret_cast<const pair*>(s + h.ec + 2 * j);
+  };
+  // the tile's planes and its B and C out of what was fetched
+  auto stage = [&](int k0, int st) {
+#pragma unroll
+    for (int p = 0; p < CHUNKS; ++p) {
+      const Chunk h = chunk(p);
+      if (h.es >= STEPS) continue;
+      pair dt[4] = {}, x[4] = {}, dv[4] = {};
+      if (h.here && k0 + h.es < stop) {
+        pair bias[4];
+        unpack_pairs<8>(raw_chunk(st, 1, p), dt);
+        unpack_pairs<8>(raw_chunk(st, 0, p), x);
+        unpack_pairs<8>(raw_chunk(st, 2, p), dv);
+        channel_values(s_bias, h, bias);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          dt[j] = add2(dt[j], bias[j]);
+          if (a.softplus) dt[j] = softplus2(dt[j]);
+          x[j] = mul2(x[j], dt[j]);
+        }
+        if (GATE) {
+          pair z[4];
+          unpack_pairs<8>(raw_chunk(st, 3, p), z);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) dv[j] = mul2(dv[j], mul2(z[j], sigmoid2(z[j])));
+        }
+      }
+      to_plane(s_dt, h, dt);
+      to_plane(s_x, h, x);
+      to_plane(s_dv, h, dv);
+    }
+#pragma unroll
+    for (int i = 0; i < QB; ++i) {
+      const int q = tid + i * NT, n4 = (q % (NP / 4)) * 4, which = (q / (NP / 4)) & 1, step = q / (NP / 2);
+      if (q >= S::QUARTERS) continue;
+      float f[4] = {0, 0, 0, 0};
+      if (k0 + step < stop && n4 < a.states) {
+        Raw<T, 4> r;
+        memcpy(&r, reinterpret_cast<const uint8_t*>(s_raw + (st * S::PIECES + 4 * S::ARRAY) * NT) + (size_t)q * 4 * sizeof(T), sizeof r);
+        unpack<4>(r, f);
+      }
+      const int half = (n4 / 4) & 1, at_lane = n4 / PER_LANE;
+#pragma unroll
+      for (int o = 0; o < S::ORDERS; ++o) {
+        // order o exchanges the halves (bit 1) and the pairs of a half (bit 0)
+        float* const to = s_bc + (step * 2 + which) * S::ROW + (((half ^ (o >> 1)) * S::ORDERS + o) * LANES + at_lane) * 4;
+        *reinterpret_cast<float4*>(to) = o & 1 ? make_float4(f[2], f[3], f[0], f[1]) : make_float4(f[0], f[1], f[2], f[3]);
+      }
+    }
   };
   // state s over step k of the tile: returns its decays
   auto advance = [&](pair (&s)[4], float dt, float x, int k, pair (&e)[4]) {
@@ -181,97 +324,79 @@ __global__ void __launch_bounds__(NT, 3) scan_bwd(const ScanArgs a) {
       s[i] = fma2(e[i], s[i], mul2(both(x), B[i]));
     }
   };
-
-  const int tiles = (last - first + TILE - 1) / TILE;
-  const int busy = n <= first ? 0 : min(tiles, (n - first + TILE - 1) / TILE);
-  for (int i = tiles - 1; i >= 0; --i) {
-    const int k0 = first + i * TILE, steps = min(TILE, min(n, last) - k0);
-    if (i >= busy) {
-      // behind the row's last step: zeros (dB and dC of these steps are the second kernel's)
-      const float zero[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  auto forwards = [&](pair (&s)[4], int from, int to) {
+    for (int k = from; k < to; k += 4) {
+      float dt[4], x[4];
+      At::four(s_dt, c, k, dt);
+      At::four(s_x, c, k, x);
 #pragma unroll
-      for (int p = 0; p < CHUNKS; ++p) {
-        const Chunk h = chunk(p, k0);
-        if (h.es >= TILE || h.en <= 0 || k0 + h.es >= last) continue;
-        write(a.du, a.pu, h, k0, zero);
-        write(a.ddelta, a.pd, h, k0, zero);
-        if (GATE) write(a.dz, a.pz, h, k0, zero);
+      for (int j = 0; j < 4; ++j) {
+        pair e[4];
+        advance(s, dt[j], x[j], k + j, e);
       }
-      continue;
     }
-    __syncthreads();                              // the tile before has been read
+  };
+  // The state before a tile that a visit to the tile before it has found: in the place of a kept state that this spacing never has.
+  auto found = [&](bool put, pair (&s)[4]) {
+    pair* const p = reinterpret_cast<pair*>(s_raw + tid + (4 * S::ARRAY + S::BC + 2) * NT);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (put) p[(i >> 1) * 2 * NT + (i & 1)] = s[i];
+      else s[i] = p[(i >> 1) * 2 * NT + (i & 1)];
+    }
+  };
+
+  const int tiles = (last - first + STEPS - 1) / STEPS;
+  const int busy = n <= first ? 0 : min(tiles, (n - first + STEPS - 1) / STEPS);
+  // behind the row's last step: zeros (dB and dC of these steps are the second kernel's)
+  for (int i = busy; i < tiles; ++i) {
+    const pair zero[4] = {};
 #pragma unroll
     for (int p = 0; p < CHUNKS; ++p) {
-      const Chunk h = chunk(p, k0);
-      if (h.es >= TILE) continue;
-      float fu[8], pre[8], dv[8], z[8];
-      unpack<8>(read(a.u, a.pu, h, k0), fu);
-      unpack<8>(read(a.delta, a.pd, h, k0), pre);
-      unpack<8>(read(a.dy, a.py, h, k0), dv);
-      if (GATE) unpack<8>(read(a.z, a.pz, h, k0), z);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int w = At::at(h.ec + j, h.es);
-        const float dt = h.in ? step_size(pre[j] + s_bias[h.ec + j], a.softplus) : 0.f;
-        s_dt[w] = dt;
-        s_x[w] = h.in ? dt * fu[j] : 0.f;
-        s_dv[w] = !h.in ? 0.f : GATE ? dv[j] * z[j] * sigmoid(z[j]) : dv[j];
-      }
+      const Chunk h = chunk(p);
+      const int k0 = first + i * STEPS;
+      if (!h.here || k0 + h.es >= last) continue;
+      write(a.du, a.pu, h, k0, zero);
+      write(a.ddelta, a.pd, h, k0, zero);
+      if (GATE) write(a.dz, a.pz, h, k0, zero);
     }
-    for (int q = tid; q < TILE * NP / 2; q += NT) {
-      const int n4 = (q % (NP / 4)) * 4, which = (q / (NP / 4)) & 1, step = q / (NP / 2), k = k0 + step;
-      float f[4] = {0, 0, 0, 0};
-      if (k < n && k < last && n4 < a.states)
-        unpack<4>(load_raw<4>((which ? Cm + (int64_t)k * a.pc.step : Bm + (int64_t)k * a.pb.step) + n4, a.states - n4, a.vec_s && n4 + 4 <= a.states), f);
-      const int half = (n4 / 4) & 1, at_lane = n4 / PER_LANE;
-#pragma unroll
-      for (int o = 0; o < S::ORDERS; ++o) {
-        // order o exchanges the halves (bit 1) and the pairs of a half (bit 0)
-        float* const to = s_bc + (step * 2 + which) * S::ROW + (((half ^ (o >> 1)) * S::ORDERS + o) * LANES + at_lane) * 4;
-        *reinterpret_cast<float4*>(to) = o & 1 ? make_float4(f[2], f[3], f[0], f[1]) : make_float4(f[0], f[1], f[2], f[3]);
-      }
-    }
-    // the state before the tile; with states kept further apart than eight steps, those before its other eights
-    pair s0[4] = {};
-    if (mine) load_turned(a.kept + (int64_t)(k0 / a.spacing) * layer + place, l, turn, NP, true, s0);
+  }
+  // Tiles from the last to the first.  With states kept every 32 steps an odd tile's first state is found by a visit to the even
+  // tile before it.  (Segments begin at multiples of 32.)
+  auto needs_visit = [&](int i) { return a.spacing > STEPS && (i & 1); };
+  int i = busy - 1, st = 0;
+  bool visit = i >= 0 && needs_visit(i);
+  if (i >= 0) fetch(first + (visit ? i - 1 : i) * STEPS, st);
+  while (i >= 0) {
+    const int k0 = first + (visit ? i - 1 : i) * STEPS, steps = min(STEPS, stop - k0);
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    __syncthreads();                              // the tile before has been read
+    stage(k0, st);
+    const int next = visit ? i : i - 1;
+    const bool next_visit = !visit && next >= 0 && needs_visit(next);
+    if (next >= 0) fetch(first + (next_visit ? next - 1 : next) * STEPS, st ^ 1);
+    else asm volatile("cp.async.commit_group;" ::: "memory");
     __syncthreads();
-    if (a.spacing > EIGHT) {
-      pair s[4] = {s0[0], s0[1], s0[2], s0[3]};
-      for (int e = 0; (e + 1) * EIGHT < steps; ++e) {
-        if (((e + 1) * EIGHT & (a.spacing - 1)) == 0) {
-          if (mine) load_turned(a.kept + (int64_t)((k0 + (e + 1) * EIGHT) / a.spacing) * layer + place, l, turn, NP, true, s);
-        } else {
-#pragma unroll
-          for (int j0 = 0; j0 < EIGHT; j0 += 4) {
-            float dt[4], x[4];
-            At::four(s_dt, c, e * EIGHT + j0, dt);
-            At::four(s_x, c, e * EIGHT + j0, x);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              pair decay[4];
-              advance(s, dt[j], x[j], e * EIGHT + j0 + j, decay);
-            }
-          }
-        }
-#pragma unroll
-        for (int q = 0; q < 4; ++q) *reinterpret_cast<pair*>(s_start + (e * NT + tid) * PER_LANE + 2 * q) = s[q];
-      }
+    if (visit) {
+      pair s[4];
+      kept_state(st, 0, s);
+      forwards(s, 0, STEPS);
+      found(true, s);
+      visit = false;
+      st ^= 1;
+      continue;
     }
+    auto before = [&](int e, pair (&s)[4]) {      // the state before an eight
+      if (((k0 + e * EIGHT) & (a.spacing - 1)) == 0) return kept_state(st, e, s);
+      if ((k0 & (a.spacing - 1)) == 0) kept_state(st, 0, s);
+      else found(false, s);
+      if (e > 0) forwards(s, 0, EIGHT);
+    };
     pair tA[4] = {};
-    const int eights = (steps + EIGHT - 1) / EIGHT;
-    for (int e = eights - 1; e >= 0; --e) {
+    for (int e = steps > EIGHT ? 1 : 0; e >= 0; --e) {
       pair decay[EIGHT][4], state[EIGHT + 1][4];  // of a step; before it
-#pragma unroll
-      for (int q = 0; q < 4; ++q) state[0][q] = s0[q];
-      if (e > 0) {
-        if (a.spacing > EIGHT) {
-#pragma unroll
-          for (int q = 0; q < 4; ++q) state[0][q] = *reinterpret_cast<const pair*>(s_start + ((e - 1) * NT + tid) * PER_LANE + 2 * q);
-        } else if (mine) {
-          load_turned(a.kept + (int64_t)(k0 / EIGHT + e) * layer + place, l, turn, NP, true, state[0]);
-        }
-      }
-      float* const red = s_red + (e & 1) * S::RED + warp * EIGHT * 2 * NP;
+      before(e, state[0]);
+      float* const red = s_red + warp * EIGHT * 2 * NP;
 #pragma unroll
       for (int j0 = 0; j0 < EIGHT; j0 += 4) {
         float dt[4], x[4];
@@ -298,7 +423,7 @@ __global__ void __launch_bounds__(NT, 3) scan_bwd(const ScanArgs a) {
           const ulonglong2 c0 = *reinterpret_cast<const ulonglong2*>(p + S::ROW), c1 = *reinterpret_cast<const ulonglong2*>(p + S::ROW + 16 * LANES);
           const pair B[4] = {b0.x, b0.y, b1.x, b1.y}, C[4] = {c0.x, c0.y, c1.x, c1.y};
           const pair (&after)[4] = state[j0 + j + 1];
-          const pair (&before)[4] = state[j0 + j];
+          const pair (&at_start)[4] = state[j0 + j];
           const pair x2 = both(x[j]), v2 = both(dv[j]), dt2 = both(dt[j]);
           if (GATE) sv[j] = dot(C, after);
           pair G[4], dB[4], dC[4];
@@ -312,7 +437,7 @@ __global__ void __launch_bounds__(NT, 3) scan_bwd(const ScanArgs a) {
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
             carry[q] = mul2(decay[j0 + j][q], G[q]);
-            G[q] = mul2(carry[q], before[q]);      // g a s_{k-1}
+            G[q] = mul2(carry[q], at_start[q]);    // g a s_{k-1}
             tA[q] = fma2(dt2, G[q], tA[q]);
           }
           sA[j] = dot(G, A);
@@ -331,45 +456,59 @@ __global__ void __launch_bounds__(NT, 3) scan_bwd(const ScanArgs a) {
       // this eight's sums over the block's channels
       for (int q = tid; q < EIGHT * 2 * NP; q += NT) {
         const int j = q / (2 * NP), k = k0 + e * EIGHT + j;
-        if (k >= n || k >= last) continue;
+        if (k >= stop) continue;
         float v = 0.f;
 #pragma unroll
-        for (int w = 0; w < WARPS; ++w) v += s_red[(e & 1) * S::RED + w * EIGHT * 2 * NP + q];
+        for (int w = 0; w < WARPS; ++w) v += s_red[w * EIGHT * 2 * NP + q];
         a.part_bc[((((int64_t)block * a.t + k) * a.batch + b) * a.groups + g) * 2 * NP + q % (2 * NP)] = v;
       }
+      if (e > 0) __syncthreads();                 // they have been read
     }
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       pair* const sum = reinterpret_cast<pair*>(s_dA + tid * PER_LANE + 2 * q);
       *sum = add2(*sum, tA[q]);
     }
-    __syncthreads();
 #pragma unroll
     for (int p = 0; p < CHUNKS; ++p) {
-      const Chunk h = chunk(p, k0);
-      if (h.es >= TILE) continue;
-      float fu[8], pre[8], dy[8], z[8], du[8], dd[8], dz[8];
-      unpack<8>(read(a.u, a.pu, h, k0), fu);
-      unpack<8>(read(a.delta, a.pd, h, k0), pre);
-      unpack<8>(read(a.dy, a.py, h, k0), dy);
-      if (GATE) unpack<8>(read(a.z, a.pz, h, k0), z);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int w = At::at(h.ec + j, h.es);
-        const float skip = s_skip[h.ec + j];
-        float dv = dy[j];
+      const Chunk h = chunk(p);
+      if (h.es >= STEPS) continue;
+      pair du[4] = {}, dd[4] = {}, dz[4] = {}, vu[4] = {};
+      if (h.here && k0 + h.es < stop) {
+        pair skip[4], bias[4], u[4], dv[4];
+        channel_values(s_skip, h, skip);
+        channel_values(s_bias, h, bias);
+        unpack_pairs<8>(raw_chunk(st, 0, p), u);
+        unpack_pairs<8>(raw_chunk(st, 1, p), dd);
+        unpack_pairs<8>(raw_chunk(st, 2, p), dv);
         if (GATE) {
-          const float sig = sigmoid(z[j]);
-          dv = dy[j] * z[j] * sig;
-          dz[j] = h.in ? dy[j] * fmaf(skip, fu[j], s_v[w]) * dsilu(z[j], sig) : 0.f;
+          pair z[4], v[4];
+          unpack_pairs<8>(raw_chunk(st, 3, p), z);
+          plane(s_v, h, v);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const pair sig = sigmoid2(z[j]), zs = mul2(z[j], sig);
+            // silu' = s + z s (1 - s)
+            const pair f = fma2(zs, fma2(sig, both(-1.f), both(1.f)), sig);
+            dz[j] = mul2(mul2(dv[j], fma2(skip[j], u[j], v[j])), f);
+            dv[j] = mul2(dv[j], zs);
+          }
         }
-        const float gB = s_x[w];
-        du[j] = h.in ? fmaf(skip, dv, s_dt[w] * gB) : 0.f;
-        dd[j] = h.in ? fmaf(fu[j], gB, s_dv[w] * (1.f / kLog2e)) * (a.softplus ? sigmoid(pre[j] + s_bias[h.ec + j]) : 1.f) : 0.f;   // A is in units of log 2
-        s_x[w] = h.in ? dv * fu[j] : 0.f;
-        s_dv[w] = dd[j];
+        pair gB[4], gA[4], dt[4];
+        plane(s_x, h, gB);
+        plane(s_dv, h, gA);
+        plane(s_dt, h, dt);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          du[j] = fma2(skip[j], dv[j], mul2(dt[j], gB[j]));
+          const pair ddt = fma2(u[j], gB[j], mul2(gA[j], both(1.f / kLog2e)));        // A is in units of log 2
+          dd[j] = a.softplus ? mul2(ddt, sigmoid2(add2(dd[j], bias[j]))) : ddt;
+          vu[j] = mul2(dv[j], u[j]);
+        }
       }
-      if (h.en > 0 && k0 + h.es < last) {
+      to_plane(s_x, h, vu);
+      to_plane(s_dv, h, dd);
+      if (h.here && k0 + h.es < last) {
         write(a.du, a.pu, h, k0, du);
         write(a.ddelta, a.pd, h, k0, dd);
         if (GATE) write(a.dz, a.pz, h, k0, dz);
@@ -378,17 +517,28 @@ __global__ void __launch_bounds__(NT, 3) scan_bwd(const ScanArgs a) {
     __syncthreads();
     {
       float v = 0.f, w = 0.f;
+      if constexpr (LANES <= 4) {
 #pragma unroll
-      for (int q = 0; q < TILE / 4 / LANES; ++q) {
-        float x[4], y[4];
-        At::four(s_x, c, (q * LANES + l) * 4, x);
-        At::four(s_dv, c, (q * LANES + l) * 4, y);
-        v += (x[0] + x[1]) + (x[2] + x[3]);
-        w += (y[0] + y[1]) + (y[2] + y[3]);
+        for (int q = 0; q < STEPS / 4 / LANES; ++q) {
+          float x[4], y[4];
+          At::four(s_x, c, (q * LANES + l) * 4, x);
+          At::four(s_dv, c, (q * LANES + l) * 4, y);
+          v += (x[0] + x[1]) + (x[2] + x[3]);
+          w += (y[0] + y[1]) + (y[2] + y[3]);
+        }
+      } else {
+#pragma unroll
+        for (int q = 0; q < STEPS / LANES; ++q) {
+          v += s_x[At::at(c, q * LANES + l)];
+          w += s_dv[At::at(c, q * LANES + l)];
+        }
       }
       dskip += v;
       dbias += w;
     }
+    i = next;
+    visit = next_visit;
+    st ^= 1;
   }
 #pragma unroll
   for (int m = 1; m < LANES; m *= 2) {
@@ -459,7 +609,7 @@ __global__ void __launch_bounds__(256) scan_sums(const Sums a) {
 
 template <class T, int LANES, bool GATE>
 bool launch_gate(const ScanArgs& a, cudaStream_t s) {
-  const int bytes = (Shape<LANES>::FLOATS + (a.spacing > EIGHT ? Shape<LANES>::STARTS : 0)) * 4;
+  constexpr int bytes = Shape<T, LANES>::FLOATS * 4;
   // per call: function attributes belong to the current device
   if (cudaFuncSetAttribute(scan_bwd<T, LANES, GATE>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
   const dim3 grid((unsigned)(a.groups * a.blocks), (unsigned)a.batch, (unsigned)a.segments);

@@ -171,6 +171,22 @@ __device__ __forceinline__ pair sigmoid2(pair x) {
   const float2 d = unpack2(add2(pack2(ex2(e.x), ex2(e.y)), both(1.f)));
   return pack2(rcp(d.x), rcp(d.y));
 }
+__device__ __forceinline__ pair softplus2(pair x) {
+  const float2 f = unpack2(x);
+  const float2 y = unpack2(mul2(pack2(fabsf(f.x), fabsf(f.y)), both(-kLog2e)));
+  const pair e = pack2(ex2(y.x), ex2(y.y));
+  const float2 w = unpack2(add2(e, both(2.f)));
+  const pair t = mul2(e, pack2(rcp(w.x), rcp(w.y))), q = mul2(t, t);
+  pair p = both(1.f / 15.f);
+  p = fma2(p, q, both(1.f / 13.f));
+  p = fma2(p, q, both(1.f / 11.f));
+  p = fma2(p, q, both(1.f / 9.f));
+  p = fma2(p, q, both(1.f / 7.f));
+  p = fma2(p, q, both(1.f / 5.f));
+  p = fma2(p, q, both(1.f / 3.f));
+  p = fma2(p, q, both(1.f));
+  return fma2(add2(t, t), p, pack2(fmaxf(f.x, 0.f), fmaxf(f.y, 0.f)));
+}
 // pairs of N elements as they lie in memory
 template <int N>
 __device__ __forceinline__ void unpack_pairs(const Raw<bf16, N>& r, pair (&f)[N / 2]) {
