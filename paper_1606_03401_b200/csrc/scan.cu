@@ -13,10 +13,10 @@ namespace {
 
 // Steps of a segment and their number, for a kernel of `blocks` blocks a segment of which the device holds `room` at once.
 // Segments cost a kernel in front that walks the steps once more (backward: a lighter one), so that two of them gain little;
-// a segment has 64 steps at least, and there are 64 at most (each block folds what the others hand it).
+// a segment has 32 steps at least, and there are 64 at most (each block folds what the others hand it).
 void cut(int64_t t, int64_t blocks, int64_t room, int& segment, int& segments) {
   int64_t n = room / blocks;
-  if (n > t / 64) n = t / 64;
+  if (n > t / TILE) n = t / TILE;
   if (n > 64) n = 64;
   if (n < 2) n = 1;
   int64_t len = (t + n - 1) / n;
@@ -48,7 +48,7 @@ bool check(const mebptt_scan_desc* d, ScanArgs& a, Cut& c) {
   c.blocks_f = (a.gchannels + chf - 1) / chf;
   c.blocks_b = (a.gchannels + chb - 1) / chb;
   cut(d->t, (int64_t)d->groups * c.blocks_f * d->batch, SMS * 4, c.segment_f, c.segments_f);
-  cut(d->t, (int64_t)d->groups * c.blocks_b * d->batch, SMS * 3, c.segment_b, c.segments_b);
+  cut(d->t, (int64_t)d->groups * c.blocks_b * d->batch, SMS * 4, c.segment_b, c.segments_b);
   return true;
 }
 // What a grid can count.

@@ -1,10 +1,10 @@
 // Selective state space scan, backward.
 //
-// A block owns 128 / LANES channels of one row and walks a segment's tiles of 16 steps from the last to the first; LANES lanes share
-// a channel, eight states each, two to an instruction.  States are not kept but every `spacing` steps: eight steps at a time are
-// run forwards from the state before them, with the decays and the states of the eight steps in registers, and then backwards.
-// Where states are kept further apart, those between are found by running forwards once more.  Every thread fetches the next
-// tile's inputs and states while a tile is worked on (12 warps an SM would not hide them).
+// A block owns 128 / LANES channels of one row and walks a segment's tiles of 8 steps from the last to the first; LANES lanes share
+// a channel, eight states each, two to an instruction.  A tile runs forwards from the state before it, with the states of its
+// steps in registers, and then backwards.  States are not kept but every `spacing` steps: where that is more than a tile, the tiles
+// from one kept state to the next are first visited in ascending order to find those between.  Every thread fetches the
+// next tile's inputs and kept state while a tile is worked on.
 //
 // Sums go three ways.  Over the states of a channel (v, g B, A a s g): the lanes of a channel, four steps at a time, each lane ending
 // with steps of its own.  Over channels (dB, dC): halving exchanges among the lanes of a warp with the same states, then the
@@ -15,7 +15,7 @@
 // that keep the upper half hold it where the others hold the lower one.  So lanes hold their states in one of four orders
 // (`turn`), B and C lie in shared memory in all four, and the first two exchanges need no selections.
 //
-// Bound by instruction issue: two exponentials and some 24 other instructions for eight states of a step, and two shuffles.
+// Bound by instruction issue and the latency of its chains.
 #include <cuda_runtime.h>
 
 #include <cstdint>
@@ -30,23 +30,25 @@ namespace seq {
 
 namespace {
 
-constexpr int EIGHT = 8, NT = 128, STEPS = 16;     // steps of a tile
+constexpr int NT = 128, STEPS = 8, GW = 4;         // threads; steps of a tile; channels of a group in the elementwise parts
 
 template <class T, int LANES>
 struct Shape {
   static constexpr int CH = NT / LANES, NP = PER_LANE * LANES, WARPS = NT / 32;
-  static constexpr int CHUNKS = STEPS * CH / 8 > NT ? STEPS * CH / 8 / NT : 1;      // groups of eight channels a thread, in the elementwise part
+  static constexpr int GROUPS = STEPS * CH / GW;
+  static constexpr int QG = GROUPS > NT ? GROUPS / NT : 1;                          // groups of a thread
   static constexpr int QUARTERS = STEPS * NP / 2;                                   // of B and C: four states each
   static constexpr int QB = QUARTERS > NT ? QUARTERS / NT : 1;                      // of a thread
   using At = Tile<STEPS, CH>;
   static constexpr int ORDERS = 4;                                                  // of B and C
   static constexpr int ROW = ORDERS * NP;                                           // of B or C, of a step
-  static constexpr int RED = WARPS * EIGHT * 2 * NP;                                // sums of one eight, by warp
-  // What a thread fetches for a tile, in 16-byte pieces: u, delta, dy, z; B and C; two states.  Each thread reads what it fetched itself.
-  static constexpr int ARRAY = CHUNKS * (int)sizeof(T) / 2, BC = QB * (int)sizeof(T) / 4 > 0 ? QB * (int)sizeof(T) / 4 : 1;
-  static constexpr int PIECES = 4 * ARRAY + BC + 4;
-  // planes of the tile, B and C, sums of an eight and of tiles, the channels' bias and skip, what is fetched (twice)
-  static constexpr int FLOATS = 4 * At::FLOATS + STEPS * 2 * ROW + RED + NT * PER_LANE + 2 * CH + 2 * PIECES * NT * 4;
+  static constexpr int RED = WARPS * STEPS * 2 * NP;                                // sums over channels, by warp
+  // What threads fetch for a tile, in bytes: u, delta, dy, z (twice); B and C; a state.  Each thread reads what it fetched itself.
+  static constexpr int ARRAY = QG * NT * GW * (int)sizeof(T), BC = QB * NT * 4 * (int)sizeof(T), STATE = NT * PER_LANE * 4;
+  static constexpr int RAW = 2 * 4 * ARRAY + BC + STATE;
+  // those, planes of the tile, B and C, sums over channels, of tiles, the channels' bias and skip
+  static constexpr int BYTES = RAW + 4 * (4 * At::FLOATS + STEPS * 2 * ROW + RED + NT * PER_LANE + 2 * CH);
+  static constexpr int STARTS = (TILE / STEPS - 1) * STATE;                         // states before the tiles between those that are kept
 };
 
 // Sums of dB and dC (eight values each) over the 32 / LANES lanes with the same states.  Lanes halve the values among them as long as
@@ -103,23 +105,41 @@ __device__ __forceinline__ void async16(void* dst, const void* src) {
 __device__ __forceinline__ void async8(void* dst, const void* src) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src) : "memory");
 }
+// Four elements: asked for where they load as one, else loaded.
+template <class T>
+__device__ __forceinline__ void fetch4(uint8_t* to, const T* from, int n, bool whole) {
+  if (whole) {
+    if constexpr (sizeof(T) == 2) async8(to, from);
+    else async16(to, from);
+  } else {
+    const Raw<T, 4> r = load_raw<4>(from, n, false);
+    memcpy(to, &r, sizeof r);
+  }
+}
+template <class T>
+__device__ __forceinline__ Raw<T, 4> fetched4(const uint8_t* from) {
+  return load_raw<4>(reinterpret_cast<const T*>(from), 4, true);
+}
 
 template <class T, int LANES, bool GATE>
-__global__ void __launch_bounds__(NT, 3) scan_bwd(const ScanArgs a) {
+__global__ void __launch_bounds__(NT, 4) scan_bwd(const ScanArgs a) {
   using S = Shape<T, LANES>;
   using At = typename S::At;
-  constexpr int CH = S::CH, NP = S::NP, WARPS = S::WARPS, CHUNKS = S::CHUNKS, QB = S::QB;
-  extern __shared__ __align__(16) float sm[];
-  uint4* const s_raw = reinterpret_cast<uint4*>(sm);                                // [2][PIECES][NT]
-  float* const s_dt = sm + 2 * S::PIECES * NT * 4;   // dt
+  constexpr int CH = S::CH, NP = S::NP, WARPS = S::WARPS, QG = S::QG, QB = S::QB, E4 = 4 * (int)sizeof(T);
+  extern __shared__ __align__(16) uint8_t smem[];
+  uint8_t* const s_arrays = smem;                                         // [2][u, delta, dy, z][groups][4]
+  uint8_t* const s_rows = s_arrays + 8 * S::ARRAY;                        // [STEPS][B, C][NP], as in memory
+  float* const s_state = reinterpret_cast<float*>(s_rows + S::BC);        // [NT][8]: the state before the next tile, in two halves
+  float* const s_dt = s_state + NT * PER_LANE;    // dt
   float* const s_x = s_dt + At::FLOATS;           // dt u, then the sums over states of g B, then dv u
   float* const s_dv = s_x + At::FLOATS;           // dv, then of A a s g, then ddelta
   float* const s_v = s_dv + At::FLOATS;           // of C s
   float* const s_bc = s_v + At::FLOATS;           // [STEPS][B, C][two halves of a lane's states][orders][LANES][4]
-  float* const s_red = s_bc + STEPS * 2 * S::ROW; // [WARPS][EIGHT][2 NP]
+  float* const s_red = s_bc + STEPS * 2 * S::ROW; // [WARPS][STEPS][2 NP]
   float* const s_dA = s_red + S::RED;             // [NT][8]: sums of the tiles so far
   float* const s_bias = s_dA + NT * PER_LANE;     // [CH]
   float* const s_skip = s_bias + CH;              // [CH]
+  float* const s_start = s_skip + CH;             // [3][NT][8]: states before the tiles between those that are kept
 
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, b = blockIdx.y, seg = blockIdx.z;
   const int g = blockIdx.x / a.blocks, block = blockIdx.x % a.blocks, base = block * CH;
@@ -159,134 +179,102 @@ __global__ void __launch_bounds__(NT, 3) scan_bwd(const ScanArgs a) {
   }
   float dskip = 0.f, dbias = 0.f;
 
-  // eight channels of a step, in the elementwise parts
-  struct Chunk {
-    int ec, es, en;
-    bool here, whole;
+  // four channels of a step, in the elementwise parts
+  struct Group {
+    int c, step, n;
+    bool there, whole;
   };
-  auto chunk = [&](int p) {
+  auto group = [&](int p) {
     const int q = tid + p * NT;
-    Chunk h;
-    h.ec = (q % (CH / 8)) * 8;
-    h.es = q / (CH / 8);
-    h.en = min(8, live - h.ec);
-    h.here = h.es < STEPS && h.en > 0;
-    h.whole = a.vec_d && h.en == 8;
+    Group h;
+    h.c = (q % (CH / GW)) * GW;
+    h.step = q / (CH / GW);
+    h.n = min(GW, live - h.c);
+    h.there = h.step < STEPS && h.n > 0;
+    h.whole = a.vec_d && h.n == GW;
     return h;
   };
-  // Asks for the tile at k0: into the thread's own pieces of stage st.  Where groups do not load as one they come by plain loads.
-  auto fetch = [&](int k0, int st) {
-    uint4* const raw = s_raw + st * S::PIECES * NT + tid;
-    auto array = [&](const void* x, const Places& p, int which) {
+  // Asks for the tile at k0, arrays into half `to`.  kept: and for the state before it.
+  auto fetch = [&](int k0, int to, bool kept) {
 #pragma unroll
-      for (int q = 0; q < CHUNKS; ++q) {
-        const Chunk h = chunk(q);
-        if (!h.here || k0 + h.es >= stop) continue;
-        const T* const from = (const T*)x + (int64_t)(k0 + h.es) * p.step + (int64_t)b * p.row + d0 + h.ec;
-        uint4* const to = raw + (which * S::ARRAY + q * (int)sizeof(T) / 2) * NT;
-        if (h.whole) {
-#pragma unroll
-          for (int i = 0; i < (int)sizeof(T) / 2; ++i) async16(to + i * NT, reinterpret_cast<const uint4*>(from) + i);
-        } else {
-          const Raw<T, 8> r = load_raw<8>(from, h.en, false);
-#pragma unroll
-          for (int i = 0; i < (int)sizeof(T) / 2; ++i) to[i * NT] = make_uint4(r.w[4 * i], r.w[4 * i + 1], r.w[4 * i + 2], r.w[4 * i + 3]);
-        }
-      }
-    };
-    array(a.u, a.pu, 0);
-    array(a.delta, a.pd, 1);
-    array(a.dy, a.py, 2);
-    if (GATE) array(a.z, a.pz, 3);
-    uint8_t* const bc = reinterpret_cast<uint8_t*>(raw - tid + 4 * S::ARRAY * NT);
+    for (int q = 0; q < QG; ++q) {
+      const Group h = group(q);
+      if (!h.there || k0 + h.step >= stop) continue;
+      uint8_t* const at = s_arrays + to * 4 * S::ARRAY + (tid + q * NT) * E4;
+      auto array = [&](const void* x, const Places& p, int which) {
+        fetch4(at + which * S::ARRAY, (const T*)x + (int64_t)(k0 + h.step) * p.step + (int64_t)b * p.row + d0 + h.c, h.n, h.whole);
+      };
+      array(a.u, a.pu, 0);
+      array(a.delta, a.pd, 1);
+      array(a.dy, a.py, 2);
+      if (GATE) array(a.z, a.pz, 3);
+    }
 #pragma unroll
     for (int i = 0; i < QB; ++i) {
       const int q = tid + i * NT, n4 = (q % (NP / 4)) * 4, which = (q / (NP / 4)) & 1, k = k0 + q / (NP / 2);
       if (q >= S::QUARTERS || k >= stop || n4 >= a.states) continue;
-      const T* const from = (which ? Cm + (int64_t)k * a.pc.step : Bm + (int64_t)k * a.pb.step) + n4;
-      void* const to = bc + (size_t)q * 4 * sizeof(T);
-      if (a.vec_s && n4 + 4 <= a.states) {
-        if constexpr (sizeof(T) == 2) async8(to, from);
-        else async16(to, from);
-      } else {
-        const Raw<T, 4> r = load_raw<4>(from, a.states - n4, false);
-        memcpy(to, &r, sizeof r);
-      }
+      fetch4(s_rows + q * E4, (which ? Cm + (int64_t)k * a.pc.step : Bm + (int64_t)k * a.pb.step) + n4, a.states - n4, a.vec_s && n4 + 4 <= a.states);
     }
-    if (mine) {
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int k = k0 + e * EIGHT;
-        if (k >= stop || (k & (a.spacing - 1))) continue;
-        const uint4* const from = reinterpret_cast<const uint4*>(a.kept + (int64_t)(k / a.spacing) * layer + place + PER_LANE * l);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) async16(raw + (4 * S::ARRAY + S::BC + 2 * e + i) * NT, from + i);
-      }
+    if (mine && kept) {
+      const float* const from = a.kept + (int64_t)(k0 / a.spacing) * layer + place + PER_LANE * l;
+      async16(s_state + tid * 4, from);
+      async16(s_state + (NT + tid) * 4, from + 4);
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  auto raw_chunk = [&](int st, int which, int q) {
-    const uint4* const p = s_raw + st * S::PIECES * NT + tid + (which * S::ARRAY + q * (int)sizeof(T) / 2) * NT;
-    Raw<T, 8> r;
-#pragma unroll
-    for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
-      const uint4 v = p[i * NT];
-      r.w[4 * i] = v.x; r.w[4 * i + 1] = v.y; r.w[4 * i + 2] = v.z; r.w[4 * i + 3] = v.w;
-    }
-    return r;
-  };
-  auto kept_state = [&](int st, int e, pair (&s)[4]) {       // pairs 2 i and 2 i + 1 lie in piece i
-    const pair* const p = reinterpret_cast<const pair*>(s_raw + st * S::PIECES * NT + tid + (4 * S::ARRAY + S::BC + 2 * e) * NT);
+  auto array = [&](int half, int which, int q) { return fetched4<T>(s_arrays + (half * 4 + which) * S::ARRAY + (tid + q * NT) * E4); };
+  auto kept_state = [&](pair (&s)[4]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int at = i ^ turn;
-      s[i] = mine ? p[(at >> 1) * 2 * NT + (at & 1)] : 0;
+      s[i] = mine ? *reinterpret_cast<const pair*>(s_state + ((at >> 1) * NT + tid) * 4 + (at & 1) * 2) : 0;
     }
   };
-  auto write = [&](void* x, const Places& p, const Chunk& h, int k0, const pair (&f)[4]) {
-    store_pairs<8>((T*)x + (int64_t)(k0 + h.es) * p.step + (int64_t)b * p.row + d0 + h.ec, f, h.en, h.whole);
+  auto start = [&](int j) { return reinterpret_cast<pair*>(s_start + ((j - 1) * NT + tid) * PER_LANE); };   // before tile j of those between kept states
+  auto write = [&](void* x, const Places& p, const Group& h, int k0, const pair (&f)[2]) {
+    store_pairs<4>((T*)x + (int64_t)(k0 + h.step) * p.step + (int64_t)b * p.row + d0 + h.c, f, h.n, h.whole);
   };
-  // eight values of a plane at one step
-  auto plane = [&](const float* s, const Chunk& h, pair (&f)[4]) {
+  // four values of a plane at one step
+  auto plane = [&](const float* s, const Group& h, pair (&f)[2]) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) f[j] = pack2(s[At::at(h.ec + 2 * j, h.es)], s[At::at(h.ec + 2 * j + 1, h.es)]);
+    for (int j = 0; j < 2; ++j) f[j] = pack2(s[At::at(h.c + 2 * j, h.step)], s[At::at(h.c + 2 * j + 1, h.step)]);
   };
-  auto to_plane = [&](float* s, const Chunk& h, const pair (&f)[4]) {
+  auto to_plane = [&](float* s, const Group& h, const pair (&f)[2]) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < 2; ++j) {
       const float2 v = unpack2(f[j]);
-      s[At::at(h.ec + 2 * j, h.es)] = v.x;
-      s[At::at(h.ec + 2 * j + 1, h.es)] = v.y;
+      s[At::at(h.c + 2 * j, h.step)] = v.x;
+      s[At::at(h.c + 2 * j + 1, h.step)] = v.y;
     }
   };
-  auto channel_values = [&](const float* s, const Chunk& h, pair (&f)[4]) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) f[j] = *reinterpret_cast<const pair*>(s + h.ec + 2 * j);
+  auto channel_values = [&](const float* s, const Group& h, pair (&f)[2]) {
+    const ulonglong2 v = *reinterpret_cast<const ulonglong2*>(s + h.c);
+    f[0] = v.x; f[1] = v.y;
   };
   // the tile's planes and its B and C out of what was fetched
-  auto stage = [&](int k0, int st) {
+  auto stage = [&](int k0, int half) {
 #pragma unroll
-    for (int p = 0; p < CHUNKS; ++p) {
-      const Chunk h = chunk(p);
-      if (h.es >= STEPS) continue;
-      pair dt[4] = {}, x[4] = {}, dv[4] = {};
-      if (h.here && k0 + h.es < stop) {
-        pair bias[4];
-        unpack_pairs<8>(raw_chunk(st, 1, p), dt);
-        unpack_pairs<8>(raw_chunk(st, 0, p), x);
-        unpack_pairs<8>(raw_chunk(st, 2, p), dv);
+    for (int p = 0; p < QG; ++p) {
+      const Group h = group(p);
+      if (h.step >= STEPS) continue;
+      pair dt[2] = {}, x[2] = {}, dv[2] = {};
+      if (h.there && k0 + h.step < stop) {
+        pair bias[2];
+        unpack_pairs<4>(array(half, 1, p), dt);
+        unpack_pairs<4>(array(half, 0, p), x);
+        unpack_pairs<4>(array(half, 2, p), dv);
         channel_values(s_bias, h, bias);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < 2; ++j) {
           dt[j] = add2(dt[j], bias[j]);
           if (a.softplus) dt[j] = softplus2(dt[j]);
           x[j] = mul2(x[j], dt[j]);
         }
         if (GATE) {
-          pair z[4];
-          unpack_pairs<8>(raw_chunk(st, 3, p), z);
+          pair z[2];
+          unpack_pairs<4>(array(half, 3, p), z);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) dv[j] = mul2(dv[j], mul2(z[j], sigmoid2(z[j])));
+          for (int j = 0; j < 2; ++j) dv[j] = mul2(dv[j], mul2(z[j], sigmoid2(z[j])));
         }
       }
       to_plane(s_dt, h, dt);
@@ -298,195 +286,168 @@ __global__ void __launch_bounds__(NT, 3) scan_bwd(const ScanArgs a) {
       const int q = tid + i * NT, n4 = (q % (NP / 4)) * 4, which = (q / (NP / 4)) & 1, step = q / (NP / 2);
       if (q >= S::QUARTERS) continue;
       float f[4] = {0, 0, 0, 0};
-      if (k0 + step < stop && n4 < a.states) {
-        Raw<T, 4> r;
-        memcpy(&r, reinterpret_cast<const uint8_t*>(s_raw + (st * S::PIECES + 4 * S::ARRAY) * NT) + (size_t)q * 4 * sizeof(T), sizeof r);
-        unpack<4>(r, f);
-      }
-      const int half = (n4 / 4) & 1, at_lane = n4 / PER_LANE;
+      if (k0 + step < stop && n4 < a.states) unpack<4>(fetched4<T>(s_rows + q * E4), f);
+      const int upper = (n4 / 4) & 1, at_lane = n4 / PER_LANE;
 #pragma unroll
       for (int o = 0; o < S::ORDERS; ++o) {
         // order o exchanges the halves (bit 1) and the pairs of a half (bit 0)
-        float* const to = s_bc + (step * 2 + which) * S::ROW + (((half ^ (o >> 1)) * S::ORDERS + o) * LANES + at_lane) * 4;
+        float* const to = s_bc + (step * 2 + which) * S::ROW + (((upper ^ (o >> 1)) * S::ORDERS + o) * LANES + at_lane) * 4;
         *reinterpret_cast<float4*>(to) = o & 1 ? make_float4(f[2], f[3], f[0], f[1]) : make_float4(f[0], f[1], f[2], f[3]);
       }
     }
   };
-  // state s over step k of the tile: returns its decays
-  auto advance = [&](pair (&s)[4], float dt, float x, int k, pair (&e)[4]) {
-    pair B[4];
-    const float* const p = my_bc + k * 2 * S::ROW;
+  auto lane_row = [&](const float* p, pair (&v)[4]) {
     const ulonglong2 v0 = *reinterpret_cast<const ulonglong2*>(p), v1 = *reinterpret_cast<const ulonglong2*>(p + 16 * LANES);
-    B[0] = v0.x; B[1] = v0.y; B[2] = v1.x; B[3] = v1.y;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      e[i] = decay2(both(dt), A[i]);
-      s[i] = fma2(e[i], s[i], mul2(both(x), B[i]));
-    }
-  };
-  auto forwards = [&](pair (&s)[4], int from, int to) {
-    for (int k = from; k < to; k += 4) {
-      float dt[4], x[4];
-      At::four(s_dt, c, k, dt);
-      At::four(s_x, c, k, x);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        pair e[4];
-        advance(s, dt[j], x[j], k + j, e);
-      }
-    }
-  };
-  // The state before a tile that a visit to the tile before it has found: in the place of a kept state that this spacing never has.
-  auto found = [&](bool put, pair (&s)[4]) {
-    pair* const p = reinterpret_cast<pair*>(s_raw + tid + (4 * S::ARRAY + S::BC + 2) * NT);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (put) p[(i >> 1) * 2 * NT + (i & 1)] = s[i];
-      else s[i] = p[(i >> 1) * 2 * NT + (i & 1)];
-    }
+    v[0] = v0.x; v[1] = v0.y; v[2] = v1.x; v[3] = v1.y;
   };
 
   const int tiles = (last - first + STEPS - 1) / STEPS;
   const int busy = n <= first ? 0 : min(tiles, (n - first + STEPS - 1) / STEPS);
   // behind the row's last step: zeros (dB and dC of these steps are the second kernel's)
   for (int i = busy; i < tiles; ++i) {
-    const pair zero[4] = {};
+    const pair zero[2] = {};
 #pragma unroll
-    for (int p = 0; p < CHUNKS; ++p) {
-      const Chunk h = chunk(p);
+    for (int p = 0; p < QG; ++p) {
+      const Group h = group(p);
       const int k0 = first + i * STEPS;
-      if (!h.here || k0 + h.es >= last) continue;
+      if (!h.there || k0 + h.step >= last) continue;
       write(a.du, a.pu, h, k0, zero);
       write(a.ddelta, a.pd, h, k0, zero);
       if (GATE) write(a.dz, a.pz, h, k0, zero);
     }
   }
-  // Tiles from the last to the first.  With states kept every 32 steps an odd tile's first state is found by a visit to the even
-  // tile before it.  (Segments begin at multiples of 32.)
-  auto needs_visit = [&](int i) { return a.spacing > STEPS && (i & 1); };
-  int i = busy - 1, st = 0;
-  bool visit = i >= 0 && needs_visit(i);
-  if (i >= 0) fetch(first + (visit ? i - 1 : i) * STEPS, st);
+  // Tiles from the last to the first, those between two kept states together: with `per` of them, the states before all but the first
+  // are found by visits to the tiles before them, in ascending order.  (Segments begin where states are kept.)
+  const int per = a.spacing / STEPS;
+  int i = busy - 1, half = 0;                     // the tile to be worked on
+  int visit = i >= 0 && i % per ? i - i % per : -1;   // the tile to be visited first, -1: none
+  if (i >= 0) fetch(first + (visit >= 0 ? visit : i) * STEPS, half, true);
   while (i >= 0) {
-    const int k0 = first + (visit ? i - 1 : i) * STEPS, steps = min(STEPS, stop - k0);
+    const int tile = visit >= 0 ? visit : i, k0 = first + tile * STEPS, steps = min(STEPS, stop - k0);
     asm volatile("cp.async.wait_group 0;" ::: "memory");
     __syncthreads();                              // the tile before has been read
-    stage(k0, st);
-    const int next = visit ? i : i - 1;
-    const bool next_visit = !visit && next >= 0 && needs_visit(next);
-    if (next >= 0) fetch(first + (next_visit ? next - 1 : next) * STEPS, st ^ 1);
-    else asm volatile("cp.async.commit_group;" ::: "memory");
+    pair state[STEPS + 1][4];                     // before a step
+    if (tile % per == 0) {
+      kept_state(state[0]);
+    } else {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) state[0][q] = start(tile % per)[q];
+    }
+    stage(k0, half);
+    int next = i, next_visit = visit;
+    if (visit < 0) {
+      --next;
+      next_visit = next >= 0 && next % per == per - 1 && per > 1 ? next - (per - 1) : -1;
+    } else if (++next_visit == i) {
+      next_visit = -1;
+    }
+    const int next_tile = next_visit >= 0 ? next_visit : next;
+    if (next_tile >= 0) fetch(first + next_tile * STEPS, half ^ 1, next_tile % per == 0);
     __syncthreads();
-    if (visit) {
-      pair s[4];
-      kept_state(st, 0, s);
-      forwards(s, 0, STEPS);
-      found(true, s);
-      visit = false;
-      st ^= 1;
+    // forwards
+#pragma unroll
+    for (int j0 = 0; j0 < STEPS; j0 += 4) {
+      float dt[4], x[4];
+      At::four(s_dt, c, j0, dt);
+      At::four(s_x, c, j0, x);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        pair B[4];
+        lane_row(my_bc + (j0 + j) * 2 * S::ROW, B);
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          state[j0 + j + 1][q] = fma2(decay2(both(dt[j]), A[q]), state[j0 + j][q], mul2(both(x[j]), B[q]));
+      }
+    }
+    half ^= 1;
+    if (visit >= 0) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) start(tile % per + 1)[q] = state[STEPS][q];
+      visit = next_visit;
       continue;
     }
-    auto before = [&](int e, pair (&s)[4]) {      // the state before an eight
-      if (((k0 + e * EIGHT) & (a.spacing - 1)) == 0) return kept_state(st, e, s);
-      if ((k0 & (a.spacing - 1)) == 0) kept_state(st, 0, s);
-      else found(false, s);
-      if (e > 0) forwards(s, 0, EIGHT);
-    };
+    // Backwards.  The decays are computed once more: to hold them too would leave an SM 12 warps instead of 16.  (The compiler,
+    // which would rather hold them, is told that A may be another now; and between groups of steps, that memory may be.)
+    asm volatile("" : "+l"(A[0]), "+l"(A[1]), "+l"(A[2]), "+l"(A[3])::"memory");
     pair tA[4] = {};
-    for (int e = steps > EIGHT ? 1 : 0; e >= 0; --e) {
-      pair decay[EIGHT][4], state[EIGHT + 1][4];  // of a step; before it
-      before(e, state[0]);
-      float* const red = s_red + warp * EIGHT * 2 * NP;
+    float* const red = s_red + warp * STEPS * 2 * NP;
 #pragma unroll
-      for (int j0 = 0; j0 < EIGHT; j0 += 4) {
-        float dt[4], x[4];
-        At::four(s_dt, c, e * EIGHT + j0, dt);
-        At::four(s_x, c, e * EIGHT + j0, x);
+    for (int j0 = STEPS - 4; j0 >= 0; j0 -= 4) {
+      float dt[4], x[4], dv[4], sv[4], sB[4], sA[4];
+      asm volatile("" ::: "memory");
+      At::four(s_dt, c, j0, dt);
+      At::four(s_x, c, j0, x);
+      At::four(s_dv, c, j0, dv);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+      for (int j = 3; j >= 0; --j) {
+        const float* const p = my_bc + (j0 + j) * 2 * S::ROW;
+        pair B[4], C[4], G[4], dB[4], dC[4];
+        lane_row(p, B);
+        lane_row(p + S::ROW, C);
+        const pair (&after)[4] = state[j0 + j + 1];
+        const pair x2 = both(x[j]), v2 = both(dv[j]), dt2 = both(dt[j]);
+        if (GATE) sv[j] = dot(C, after);
 #pragma unroll
-          for (int q = 0; q < 4; ++q) state[j0 + j + 1][q] = state[j0 + j][q];
-          advance(state[j0 + j + 1], dt[j], x[j], e * EIGHT + j0 + j, decay[j0 + j]);
+        for (int q = 0; q < 4; ++q) {
+          G[q] = fma2(v2, C[q], carry[q]);
+          dB[q] = mul2(x2, G[q]);
+          dC[q] = mul2(v2, after[q]);
         }
-      }
+        sB[j] = dot(G, B);
 #pragma unroll
-      for (int j0 = EIGHT - 4; j0 >= 0; j0 -= 4) {
-        const int k = e * EIGHT + j0;
-        float dt[4], x[4], dv[4], sv[4], sB[4], sA[4];
-        At::four(s_dt, c, k, dt);
-        At::four(s_x, c, k, x);
-        At::four(s_dv, c, k, dv);
-#pragma unroll
-        for (int j = 3; j >= 0; --j) {
-          const float* const p = my_bc + (k + j) * 2 * S::ROW;
-          const ulonglong2 b0 = *reinterpret_cast<const ulonglong2*>(p), b1 = *reinterpret_cast<const ulonglong2*>(p + 16 * LANES);
-          const ulonglong2 c0 = *reinterpret_cast<const ulonglong2*>(p + S::ROW), c1 = *reinterpret_cast<const ulonglong2*>(p + S::ROW + 16 * LANES);
-          const pair B[4] = {b0.x, b0.y, b1.x, b1.y}, C[4] = {c0.x, c0.y, c1.x, c1.y};
-          const pair (&after)[4] = state[j0 + j + 1];
-          const pair (&at_start)[4] = state[j0 + j];
-          const pair x2 = both(x[j]), v2 = both(dv[j]), dt2 = both(dt[j]);
-          if (GATE) sv[j] = dot(C, after);
-          pair G[4], dB[4], dC[4];
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            G[q] = fma2(v2, C[q], carry[q]);
-            dB[q] = mul2(x2, G[q]);
-            dC[q] = mul2(v2, after[q]);
-          }
-          sB[j] = dot(G, B);
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            carry[q] = mul2(decay[j0 + j][q], G[q]);
-            G[q] = mul2(carry[q], at_start[q]);    // g a s_{k-1}
-            tA[q] = fma2(dt2, G[q], tA[q]);
-          }
-          sA[j] = dot(G, A);
-          sum_channels<LANES>(dB, dC, lane);
-          put_channels<LANES>(red + (j0 + j) * 2 * NP, dB, dC, lane, l, turn);
+        for (int q = 0; q < 4; ++q) {
+          carry[q] = mul2(decay2(dt2, A[q]), G[q]);
+          G[q] = mul2(carry[q], state[j0 + j][q]);   // g a s_{k-1}
+          tA[q] = fma2(dt2, G[q], tA[q]);
         }
-        if (GATE) sum_lanes<LANES>(sv, l);
-        sum_lanes<LANES>(sB, l);
-        sum_lanes<LANES>(sA, l);
-        const int w = At::at(c, k);
-        if (GATE) put_steps<LANES>(s_v + w, l, sv);
-        put_steps<LANES>(s_x + w, l, sB);
-        put_steps<LANES>(s_dv + w, l, sA);
+        sA[j] = dot(G, A);
+        sum_channels<LANES>(dB, dC, lane);
+        put_channels<LANES>(red + (j0 + j) * 2 * NP, dB, dC, lane, l, turn);
       }
-      __syncthreads();
-      // this eight's sums over the block's channels
-      for (int q = tid; q < EIGHT * 2 * NP; q += NT) {
-        const int j = q / (2 * NP), k = k0 + e * EIGHT + j;
-        if (k >= stop) continue;
-        float v = 0.f;
-#pragma unroll
-        for (int w = 0; w < WARPS; ++w) v += s_red[w * EIGHT * 2 * NP + q];
-        a.part_bc[((((int64_t)block * a.t + k) * a.batch + b) * a.groups + g) * 2 * NP + q % (2 * NP)] = v;
-      }
-      if (e > 0) __syncthreads();                 // they have been read
+      if (GATE) sum_lanes<LANES>(sv, l);
+      sum_lanes<LANES>(sB, l);
+      sum_lanes<LANES>(sA, l);
+      const int w = At::at(c, j0);
+      if (GATE) put_steps<LANES>(s_v + w, l, sv);
+      put_steps<LANES>(s_x + w, l, sB);
+      put_steps<LANES>(s_dv + w, l, sA);
     }
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       pair* const sum = reinterpret_cast<pair*>(s_dA + tid * PER_LANE + 2 * q);
       *sum = add2(*sum, tA[q]);
     }
+    __syncthreads();
+    // this tile's sums over the block's channels
+    {
+      float* const out = a.part_bc + ((((int64_t)block * a.t + k0) * a.batch + b) * a.groups + g) * 2 * NP;
+      const int64_t step = (int64_t)a.batch * a.groups * 2 * NP;
+      for (int q = tid; q < steps * 2 * NP; q += NT) {
+        float v = 0.f;
 #pragma unroll
-    for (int p = 0; p < CHUNKS; ++p) {
-      const Chunk h = chunk(p);
-      if (h.es >= STEPS) continue;
-      pair du[4] = {}, dd[4] = {}, dz[4] = {}, vu[4] = {};
-      if (h.here && k0 + h.es < stop) {
-        pair skip[4], bias[4], u[4], dv[4];
+        for (int w = 0; w < WARPS; ++w) v += s_red[w * STEPS * 2 * NP + q];
+        out[q / (2 * NP) * step + q % (2 * NP)] = v;
+      }
+    }
+    const int was = half ^ 1;
+#pragma unroll
+    for (int p = 0; p < QG; ++p) {
+      const Group h = group(p);
+      if (h.step >= STEPS) continue;
+      pair du[2] = {}, dd[2] = {}, dz[2] = {}, vu[2] = {};
+      if (h.there && k0 + h.step < stop) {
+        pair skip[2], bias[2], u[2], dv[2], gB[2], gA[2], dt[2];
         channel_values(s_skip, h, skip);
         channel_values(s_bias, h, bias);
-        unpack_pairs<8>(raw_chunk(st, 0, p), u);
-        unpack_pairs<8>(raw_chunk(st, 1, p), dd);
-        unpack_pairs<8>(raw_chunk(st, 2, p), dv);
+        unpack_pairs<4>(array(was, 0, p), u);
+        unpack_pairs<4>(array(was, 1, p), dd);
+        unpack_pairs<4>(array(was, 2, p), dv);
         if (GATE) {
-          pair z[4], v[4];
-          unpack_pairs<8>(raw_chunk(st, 3, p), z);
+          pair z[2], v[2];
+          unpack_pairs<4>(array(was, 3, p), z);
           plane(s_v, h, v);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
+          for (int j = 0; j < 2; ++j) {
             const pair sig = sigmoid2(z[j]), zs = mul2(z[j], sig);
             // silu' = s + z s (1 - s)
             const pair f = fma2(zs, fma2(sig, both(-1.f), both(1.f)), sig);
@@ -494,12 +455,11 @@ __global__ void __launch_bounds__(NT, 3) scan_bwd(const ScanArgs a) {
             dv[j] = mul2(dv[j], zs);
           }
         }
-        pair gB[4], gA[4], dt[4];
         plane(s_x, h, gB);
         plane(s_dv, h, gA);
         plane(s_dt, h, dt);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < 2; ++j) {
           du[j] = fma2(skip[j], dv[j], mul2(dt[j], gB[j]));
           const pair ddt = fma2(u[j], gB[j], mul2(gA[j], both(1.f / kLog2e)));        // A is in units of log 2
           dd[j] = a.softplus ? mul2(ddt, sigmoid2(add2(dd[j], bias[j]))) : ddt;
@@ -508,7 +468,7 @@ __global__ void __launch_bounds__(NT, 3) scan_bwd(const ScanArgs a) {
       }
       to_plane(s_x, h, vu);
       to_plane(s_dv, h, dd);
-      if (h.here && k0 + h.es < last) {
+      if (h.there && k0 + h.step < last) {
         write(a.du, a.pu, h, k0, du);
         write(a.ddelta, a.pd, h, k0, dd);
         if (GATE) write(a.dz, a.pz, h, k0, dz);
@@ -517,7 +477,7 @@ __global__ void __launch_bounds__(NT, 3) scan_bwd(const ScanArgs a) {
     __syncthreads();
     {
       float v = 0.f, w = 0.f;
-      if constexpr (LANES <= 4) {
+      if constexpr (LANES <= 2) {
 #pragma unroll
         for (int q = 0; q < STEPS / 4 / LANES; ++q) {
           float x[4], y[4];
@@ -538,7 +498,6 @@ __global__ void __launch_bounds__(NT, 3) scan_bwd(const ScanArgs a) {
     }
     i = next;
     visit = next_visit;
-    st ^= 1;
   }
 #pragma unroll
   for (int m = 1; m < LANES; m *= 2) {
@@ -609,7 +568,7 @@ __global__ void __launch_bounds__(256) scan_sums(const Sums a) {
 
 template <class T, int LANES, bool GATE>
 bool launch_gate(const ScanArgs& a, cudaStream_t s) {
-  constexpr int bytes = Shape<T, LANES>::FLOATS * 4;
+  const int bytes = Shape<T, LANES>::BYTES + (a.spacing > STEPS ? Shape<T, LANES>::STARTS : 0);
   // per call: function attributes belong to the current device
   if (cudaFuncSetAttribute(scan_bwd<T, LANES, GATE>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
   const dim3 grid((unsigned)(a.groups * a.blocks), (unsigned)a.batch, (unsigned)a.segments);
