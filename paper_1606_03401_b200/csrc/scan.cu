@@ -47,7 +47,7 @@ bool check(const mebptt_scan_desc* d, ScanArgs& a, Cut& c) {
   c.np = 8 * lanes;
   c.blocks_f = (a.gchannels + chf - 1) / chf;
   c.blocks_b = (a.gchannels + chb - 1) / chb;
-  cut(d->t, (int64_t)d->groups * c.blocks_f * d->batch, SMS * 4, c.segment_f, c.segments_f);
+  cut(d->t, (int64_t)d->groups * c.blocks_f * d->batch, SMS * 7, c.segment_f, c.segments_f);
   cut(d->t, (int64_t)d->groups * c.blocks_b * d->batch, SMS * 4, c.segment_b, c.segments_b);
   return true;
 }
@@ -151,7 +151,7 @@ int mebptt_scan_forward(const mebptt_scan_desc* desc, const void* u, const void*
   a.dts = (float*)((char*)workspace + w.dts);
   a.segment = c.segment_f; a.segments = c.segments_f; a.blocks = c.blocks_f;
   vectors(desc, a);
-  scan_forward(a, desc->dtype == MEBPTT_BF16, (cudaStream_t)stream);
+  if (!scan_forward(a, desc->dtype == MEBPTT_BF16, (cudaStream_t)stream)) return MEBPTT_ERR_CUDA;
   return cudaGetLastError() == cudaSuccess ? MEBPTT_OK : MEBPTT_ERR_CUDA;
 }
 
@@ -176,7 +176,7 @@ int mebptt_scan_backward(const mebptt_scan_desc* desc, const void* u, const void
   vectors(desc, a);
   if (c.segments_b > 1) {
     a.blocks = c.blocks_f;
-    scan_adjoints(a, desc->dtype == MEBPTT_BF16, (cudaStream_t)stream);
+    if (!scan_adjoints(a, desc->dtype == MEBPTT_BF16, (cudaStream_t)stream)) return MEBPTT_ERR_CUDA;
   }
   a.blocks = c.blocks_b;
   if (!scan_backward(a, desc->dtype == MEBPTT_BF16, dA, dB, dC, dskip, ddelta_bias, (cudaStream_t)stream)) return MEBPTT_ERR_CUDA;

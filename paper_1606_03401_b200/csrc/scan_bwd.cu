@@ -99,28 +99,6 @@ __device__ __forceinline__ void load_turned(const float* row, int l, int turn, i
   for (int i = 0; i < 4; ++i) s[i] = load_pair(row, PER_LANE * l + pair_at(i, turn), states, vec);
 }
 
-__device__ __forceinline__ void async16(void* dst, const void* src) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src) : "memory");
-}
-__device__ __forceinline__ void async8(void* dst, const void* src) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src) : "memory");
-}
-// Four elements: asked for where they load as one, else loaded.
-template <class T>
-__device__ __forceinline__ void fetch4(uint8_t* to, const T* from, int n, bool whole) {
-  if (whole) {
-    if constexpr (sizeof(T) == 2) async8(to, from);
-    else async16(to, from);
-  } else {
-    const Raw<T, 4> r = load_raw<4>(from, n, false);
-    memcpy(to, &r, sizeof r);
-  }
-}
-template <class T>
-__device__ __forceinline__ Raw<T, 4> fetched4(const uint8_t* from) {
-  return load_raw<4>(reinterpret_cast<const T*>(from), 4, true);
-}
-
 template <class T, int LANES, bool GATE>
 __global__ void __launch_bounds__(NT, 4) scan_bwd(const ScanArgs a) {
   using S = Shape<T, LANES>;
@@ -202,7 +180,7 @@ __global__ void __launch_bounds__(NT, 4) scan_bwd(const ScanArgs a) {
       if (!h.there || k0 + h.step >= stop) continue;
       uint8_t* const at = s_arrays + to * 4 * S::ARRAY + (tid + q * NT) * E4;
       auto array = [&](const void* x, const Places& p, int which) {
-        fetch4(at + which * S::ARRAY, (const T*)x + (int64_t)(k0 + h.step) * p.step + (int64_t)b * p.row + d0 + h.c, h.n, h.whole);
+        fetch_n<4>(at + which * S::ARRAY, (const T*)x + (int64_t)(k0 + h.step) * p.step + (int64_t)b * p.row + d0 + h.c, h.n, h.whole);
       };
       array(a.u, a.pu, 0);
       array(a.delta, a.pd, 1);
@@ -213,7 +191,7 @@ __global__ void __launch_bounds__(NT, 4) scan_bwd(const ScanArgs a) {
     for (int i = 0; i < QB; ++i) {
       const int q = tid + i * NT, n4 = (q % (NP / 4)) * 4, which = (q / (NP / 4)) & 1, k = k0 + q / (NP / 2);
       if (q >= S::QUARTERS || k >= stop || n4 >= a.states) continue;
-      fetch4(s_rows + q * E4, (which ? Cm + (int64_t)k * a.pc.step : Bm + (int64_t)k * a.pb.step) + n4, a.states - n4, a.vec_s && n4 + 4 <= a.states);
+      fetch_n<4>(s_rows + q * E4, (which ? Cm + (int64_t)k * a.pc.step : Bm + (int64_t)k * a.pb.step) + n4, a.states - n4, a.vec_s && n4 + 4 <= a.states);
     }
     if (mine && kept) {
       const float* const from = a.kept + (int64_t)(k0 / a.spacing) * layer + place + PER_LANE * l;
@@ -222,7 +200,7 @@ __global__ void __launch_bounds__(NT, 4) scan_bwd(const ScanArgs a) {
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  auto array = [&](int half, int which, int q) { return fetched4<T>(s_arrays + (half * 4 + which) * S::ARRAY + (tid + q * NT) * E4); };
+  auto array = [&](int half, int which, int q) { return fetched<T, 4>(s_arrays + (half * 4 + which) * S::ARRAY + (tid + q * NT) * E4); };
   auto kept_state = [&](pair (&s)[4]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -286,7 +264,7 @@ __global__ void __launch_bounds__(NT, 4) scan_bwd(const ScanArgs a) {
       const int q = tid + i * NT, n4 = (q % (NP / 4)) * 4, which = (q / (NP / 4)) & 1, step = q / (NP / 2);
       if (q >= S::QUARTERS) continue;
       float f[4] = {0, 0, 0, 0};
-      if (k0 + step < stop && n4 < a.states) unpack<4>(fetched4<T>(s_rows + q * E4), f);
+      if (k0 + step < stop && n4 < a.states) unpack<4>(fetched<T, 4>(s_rows + q * E4), f);
       const int upper = (n4 / 4) & 1, at_lane = n4 / PER_LANE;
 #pragma unroll
       for (int o = 0; o < S::ORDERS; ++o) {

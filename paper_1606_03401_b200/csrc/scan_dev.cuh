@@ -117,6 +117,32 @@ __device__ __forceinline__ void put_steps(float* at, int l, const float (&v)[4])
 
 __device__ __forceinline__ float step_size(float pre, int soft) { return soft ? softplus(pre) : pre; }
 
+__device__ __forceinline__ void async16(void* dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src) : "memory");
+}
+__device__ __forceinline__ void async8(void* dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src) : "memory");
+}
+// N elements into shared memory, asked for where they load as one, else loaded.
+template <int N, class T>
+__device__ __forceinline__ void fetch_n(uint8_t* to, const T* from, int n, bool whole) {
+  if (whole) {
+    if constexpr (N * sizeof(T) == 8) {
+      async8(to, from);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N * (int)sizeof(T) / 16; ++i) async16(to + 16 * i, reinterpret_cast<const uint8_t*>(from) + 16 * i);
+    }
+  } else {
+    const Raw<T, N> r = load_raw<N>(from, n, false);
+    memcpy(to, &r, sizeof r);
+  }
+}
+template <class T, int N>
+__device__ __forceinline__ Raw<T, N> fetched(const uint8_t* from) {
+  return load_raw<N>(reinterpret_cast<const T*>(from), N, true);
+}
+
 // decay over a whole segment applied to a carried value; a zero stays one whatever the factor
 __device__ __forceinline__ pair carry2(pair A, float dts, pair v, pair end) {
   const float2 p = unpack2(decay2(both(dts), A)), x = unpack2(v), e = unpack2(end);

@@ -28,46 +28,37 @@ constexpr int NT = 128;
 // What a pass of the kernel computes: outputs; the states that segments end in; the adjoints that they begin with (backward in time).
 enum Pass { OUTPUTS, ENDS, ADJOINTS };
 
-template <int LANES>
+template <class T, int LANES>
 struct Shape {
   static constexpr int CH = NT / LANES;                                                      // channels of a block
   static constexpr int STEPS = LANES == 1 ? 8 : LANES == 2 ? 16 : 32;                        // of a tile: no more than a group of channels a thread
   static constexpr int NP = PER_LANE * LANES;                                                // states, with those that pad
   static constexpr int QUARTERS = STEPS * 2 * NP / 4;                                        // of the rows of B and C, four states each
-  static constexpr int PB = QUARTERS <= NT ? 1 : QUARTERS / NT;                              // of a thread
+  static constexpr int QB = QUARTERS > NT ? QUARTERS / NT : 1;                               // of a thread
   using At = Tile<STEPS, CH>;
-  static constexpr int FLOATS = 2 * At::FLOATS + STEPS * 2 * NP;
+  // What threads fetch for a tile, in bytes: three arrays, B and C.  Each thread reads what it fetched itself.
+  static constexpr int ARRAY = NT * 8 * (int)sizeof(T), ROWS = QB * NT * 4 * (int)sizeof(T), RAW = 3 * ARRAY + ROWS;
+  static constexpr int BYTES = 2 * RAW + 4 * (2 * At::FLOATS + STEPS * 2 * NP + 2 * CH);
 };
 
 template <class T, int LANES, int PASS>
-__global__ void __launch_bounds__(NT) scan_fwd(const ScanArgs a) {
-  using S = Shape<LANES>;
-  constexpr int CH = S::CH, STEPS = S::STEPS, NP = S::NP, PB = S::PB;
+__global__ void __launch_bounds__(NT, 7) scan_fwd(const ScanArgs a) {
+  using S = Shape<T, LANES>;
   using At = typename S::At;
-  __shared__ __align__(16) float sm[S::FLOATS];
-  float* const s_dt = sm;                              // [CH][STEPS]: dt, later the sums over states; ADJOINTS: dt
-  float* const s_x = sm + At::FLOATS;                  // dt u; ADJOINTS: dy times the gate
-  float* const s_bc = sm + 2 * At::FLOATS;       // [STEPS][B, C][NP]
+  constexpr int CH = S::CH, STEPS = S::STEPS, NP = S::NP, QB = S::QB, E8 = 8 * (int)sizeof(T), E4 = 4 * (int)sizeof(T);
+  extern __shared__ __align__(16) uint8_t smem[];
+  float* const s_dt = reinterpret_cast<float*>(smem + 2 * S::RAW);    // dt, later the sums over states
+  float* const s_x = s_dt + At::FLOATS;                // dt u; ADJOINTS: dy times the gate
+  float* const s_bc = s_x + At::FLOATS;                // [STEPS][B, C][NP]
+  float* const s_bias = s_bc + STEPS * 2 * NP;         // [CH]
+  float* const s_skip = s_bias + CH;                   // [CH]
 
   const int tid = threadIdx.x, b = blockIdx.y, seg = blockIdx.z + (PASS == ADJOINTS);   // segment 0 hands its adjoint to none
   const int g = blockIdx.x / a.blocks, base = (blockIdx.x % a.blocks) * CH;     // first channel, within the group
   const int d0 = g * a.gchannels + base;
   const int live = min(CH, a.gchannels - base);
   const int n = row_steps(a.lengths, b, a.t);
-  const int first = seg * a.segment, last = min(first + a.segment, a.t);
-
-  // elementwise part: eight channels of a step
-  const int ec = (tid % (CH / 8)) * 8, es = tid / (CH / 8);
-  const bool worker = es < STEPS && ec < live;
-  const int en = min(8, live - ec);
-  const bool whole = a.vec_d && en == 8;
-  const T* const u = (const T*)a.u + (int64_t)b * a.pu.row + d0 + ec;
-  const T* const delta = (const T*)a.delta + (int64_t)b * a.pd.row + d0 + ec;
-  const T* const z = a.z ? (const T*)a.z + (int64_t)b * a.pz.row + d0 + ec : nullptr;
-  const T* const dy = (const T*)a.dy + (int64_t)b * a.py.row + d0 + ec;
-  T* const y = (T*)a.y + (int64_t)b * a.py.row + d0 + ec;
-  const T* const Bm = (const T*)a.B + (int64_t)b * a.pb.row + g * a.states;
-  const T* const Cm = (const T*)a.C + (int64_t)b * a.pc.row + g * a.states;
+  const int first = seg * a.segment, last = min(first + a.segment, a.t), stop = min(n, last);
 
   // scan: a channel and eight of its states
   const int c = tid / LANES, l = tid % LANES;
@@ -102,69 +93,86 @@ __global__ void __launch_bounds__(NT) scan_fwd(const ScanArgs a) {
       for (int i = 0; i < 4; ++i) s[i] = 0;
     }
   }
-
-  float fbias[8], fskip[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int dd = d0 + ec + i;
-    fbias[i] = worker && i < en && a.bias ? a.bias[dd] : 0.f;
-    fskip[i] = PASS == OUTPUTS && worker && i < en && a.skip ? a.skip[dd] : 0.f;
+  for (int i = tid; i < CH; i += NT) {
+    s_bias[i] = a.bias && i < live ? a.bias[d0 + i] : 0.f;
+    s_skip[i] = PASS == OUTPUTS && a.skip && i < live ? a.skip[d0 + i] : 0.f;
   }
 
-  Raw<T, 8> ru, rd, rz;
-  Raw<T, 4> rbc[PB];
-  auto load = [&](int k0) {
-    const int k = k0 + es;
-    const bool in = worker && k < n && k < last;
-    rd = in ? load_raw<8>(delta + (int64_t)k * a.pd.step, en, whole) : raw_zeros<T, 8>();
-    if (PASS == ADJOINTS) ru = in ? load_raw<8>(dy + (int64_t)k * a.py.step, en, whole) : raw_zeros<T, 8>();
-    else ru = in ? load_raw<8>(u + (int64_t)k * a.pu.step, en, whole) : raw_zeros<T, 8>();
-    if (PASS != ENDS && a.z) rz = in ? load_raw<8>(z + (int64_t)k * a.pz.step, en, whole) : raw_zeros<T, 8>();
+  // elementwise part: eight channels of a step
+  const int ec = (tid % (CH / 8)) * 8, es = tid / (CH / 8), en = min(8, live - ec);
+  const bool worker = es < STEPS && en > 0, whole = a.vec_d && en == 8;
+  // asks for the tile at k0, into one half of the room
+  auto fetch = [&](int k0, int half) {
+    uint8_t* const raw = smem + half * S::RAW;
+    if (worker && k0 + es < stop) {
+      auto array = [&](const void* x, const Places& p, int which) {
+        fetch_n<8>(raw + which * S::ARRAY + tid * E8, (const T*)x + (int64_t)(k0 + es) * p.step + (int64_t)b * p.row + d0 + ec, en, whole);
+      };
+      array(a.delta, a.pd, 0);
+      if (PASS == ADJOINTS) array(a.dy, a.py, 1);
+      else array(a.u, a.pu, 1);
+      if (PASS != ENDS && a.z) array(a.z, a.pz, 2);
+    }
 #pragma unroll
-    for (int i = 0; i < PB; ++i) {
-      const int q = tid + i * NT, n4 = (q % (NP / 4)) * 4, which = (q / (NP / 4)) & 1, step = k0 + q / (NP / 2);
-      const bool used = q < S::QUARTERS && step < n && step < last && n4 < a.states && (PASS == OUTPUTS || which == (PASS == ADJOINTS));
-      const T* p = which ? Cm + (int64_t)step * a.pc.step : Bm + (int64_t)step * a.pb.step;
-      rbc[i] = used ? load_raw<4>(p + n4, a.states - n4, a.vec_s && n4 + 4 <= a.states) : raw_zeros<T, 4>();
+    for (int i = 0; i < QB; ++i) {
+      const int q = tid + i * NT, n4 = (q % (NP / 4)) * 4, which = (q / (NP / 4)) & 1, k = k0 + q / (NP / 2);
+      if (q >= S::QUARTERS || k >= stop || n4 >= a.states || (PASS != OUTPUTS && which != (PASS == ADJOINTS))) continue;
+      const T* const from = which ? (const T*)a.C + (int64_t)k * a.pc.step + (int64_t)b * a.pc.row : (const T*)a.B + (int64_t)k * a.pb.step + (int64_t)b * a.pb.row;
+      fetch_n<4>(raw + 3 * S::ARRAY + q * E4, from + g * a.states + n4, a.states - n4, a.vec_s && n4 + 4 <= a.states);
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  // the tile's planes and its B and C out of what was fetched
+  auto stage = [&](int k0, int half) {
+    const uint8_t* const raw = smem + half * S::RAW;
+    if (es < STEPS) {
+      pair dt[4] = {}, x[4] = {};
+      if (worker && k0 + es < stop) {
+        unpack_pairs<8>(fetched<T, 8>(raw + tid * E8), dt);
+        unpack_pairs<8>(fetched<T, 8>(raw + S::ARRAY + tid * E8), x);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          dt[j] = add2(dt[j], *reinterpret_cast<const pair*>(s_bias + ec + 2 * j));
+          if (a.softplus) dt[j] = softplus2(dt[j]);
+          if (PASS != ADJOINTS) x[j] = mul2(x[j], dt[j]);
+        }
+        if (PASS == ADJOINTS && a.z) {
+          pair z[4];
+          unpack_pairs<8>(fetched<T, 8>(raw + 2 * S::ARRAY + tid * E8), z);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) x[j] = mul2(x[j], mul2(z[j], sigmoid2(z[j])));
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float2 v = unpack2(dt[j]), w = unpack2(x[j]);
+        s_dt[At::at(ec + 2 * j, es)] = v.x;
+        s_dt[At::at(ec + 2 * j + 1, es)] = v.y;
+        s_x[At::at(ec + 2 * j, es)] = w.x;
+        s_x[At::at(ec + 2 * j + 1, es)] = w.y;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < QB; ++i) {
+      const int q = tid + i * NT, n4 = (q % (NP / 4)) * 4, which = (q / (NP / 4)) & 1;
+      if (q >= S::QUARTERS || (PASS != OUTPUTS && which != (PASS == ADJOINTS))) continue;
+      float f[4] = {0, 0, 0, 0};
+      if (k0 + q / (NP / 2) < stop && n4 < a.states) unpack<4>(fetched<T, 4>(raw + 3 * S::ARRAY + q * E4), f);
+      *reinterpret_cast<float4*>(s_bc + q * 4) = make_float4(f[0], f[1], f[2], f[3]);
     }
   };
 
   const int tiles = (last - first + STEPS - 1) / STEPS;
   const int busy = n <= first ? 0 : min(tiles, (n - first + STEPS - 1) / STEPS);     // tiles with a step of the row
   float dts = 0.f;
-  if (busy > 0) load(first + (PASS == ADJOINTS ? busy - 1 : 0) * STEPS);
-  for (int i = 0; i < busy; ++i) {
-    const int k0 = first + (PASS == ADJOINTS ? busy - 1 - i : i) * STEPS;
-    float fu[8], fz[8];
-    if (es < STEPS) {
-      float pre[8];
-      unpack<8>(rd, pre);
-      unpack<8>(ru, fu);
-      const bool in = k0 + es < n && k0 + es < last;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float dt = in ? step_size(pre[j] + fbias[j], a.softplus) : 0.f;
-        s_dt[At::at(ec + j, es)] = dt;
-        if (PASS != ADJOINTS) s_x[At::at(ec + j, es)] = in ? dt * fu[j] : 0.f;
-      }
-      if (PASS != ENDS && a.z) unpack<8>(rz, fz);
-      if (PASS == ADJOINTS) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) s_x[At::at(ec + j, es)] = a.z ? fu[j] * fz[j] * sigmoid(fz[j]) : fu[j];
-      }
-    }
-#pragma unroll
-    for (int q = 0; q < PB; ++q) {
-      const int e = tid + q * NT;
-      if (e < S::QUARTERS) {
-        float f[4];
-        unpack<4>(rbc[q], f);
-        *reinterpret_cast<float4*>(s_bc + e * 4) = make_float4(f[0], f[1], f[2], f[3]);
-      }
-    }
-    if (i + 1 < busy) load(PASS == ADJOINTS ? k0 - STEPS : k0 + STEPS);
+  if (busy > 0) fetch(first + (PASS == ADJOINTS ? busy - 1 : 0) * STEPS, 0);
+  __syncthreads();                                     // bias and skip are there
+  for (int i = 0, half = 0; i < busy; ++i, half ^= 1) {
+    const int k0 = first + (PASS == ADJOINTS ? busy - 1 - i : i) * STEPS, steps = min(STEPS, stop - k0);
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    stage(k0, half);
+    if (i + 1 < busy) fetch(PASS == ADJOINTS ? k0 - STEPS : k0 + STEPS, half ^ 1);
     __syncthreads();
-    const int steps = min(STEPS, min(n, last) - k0);
     for (int jj = 0; jj < steps; jj += 4) {
       const int j0 = PASS == ADJOINTS ? (steps - 1) / 4 * 4 - jj : jj;
       float dt[4], x[4], part[4];
@@ -180,9 +188,9 @@ __global__ void __launch_bounds__(NT) scan_fwd(const ScanArgs a) {
         pair in[4], C[4];
         lds8(bc + (PASS == ADJOINTS ? NP : 0), in);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const pair e = decay2(dt2, A[i]);
-          s[i] = PASS == ADJOINTS ? mul2(e, fma2(x2, in[i], s[i])) : fma2(e, s[i], mul2(x2, in[i]));
+        for (int i4 = 0; i4 < 4; ++i4) {
+          const pair e = decay2(dt2, A[i4]);
+          s[i4] = PASS == ADJOINTS ? mul2(e, fma2(x2, in[i4], s[i4])) : fma2(e, s[i4], mul2(x2, in[i4]));
         }
         if (PASS != OUTPUTS) dts += dt[j];
         if (PASS == OUTPUTS) {
@@ -197,21 +205,28 @@ __global__ void __launch_bounds__(NT) scan_fwd(const ScanArgs a) {
     }
     __syncthreads();
     if (PASS == OUTPUTS && worker && k0 + es < last) {
-      const bool in = k0 + es < n;
-      float out[8];
+      pair out[4] = {};
+      if (k0 + es < n) {
+        const uint8_t* const raw = smem + half * S::RAW;
+        pair u[4], z[4];
+        unpack_pairs<8>(fetched<T, 8>(raw + S::ARRAY + tid * E8), u);
+        if (a.z) unpack_pairs<8>(fetched<T, 8>(raw + 2 * S::ARRAY + tid * E8), z);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float v = fmaf(fskip[j], fu[j], s_dt[At::at(ec + j, es)]);
-        out[j] = !in ? 0.f : a.z ? v * fz[j] * sigmoid(fz[j]) : v;
+        for (int j = 0; j < 4; ++j) {
+          const pair v = pack2(s_dt[At::at(ec + 2 * j, es)], s_dt[At::at(ec + 2 * j + 1, es)]);
+          out[j] = fma2(*reinterpret_cast<const pair*>(s_skip + ec + 2 * j), u[j], v);
+          if (a.z) out[j] = mul2(mul2(out[j], z[j]), sigmoid2(z[j]));
+        }
       }
-      store_n<8>(y + (int64_t)(k0 + es) * a.py.step, out, en, whole);
+      store_pairs<8>((T*)a.y + (int64_t)(k0 + es) * a.py.step + (int64_t)b * a.py.row + d0 + ec, out, en, whole);
     }
   }
   if (PASS == OUTPUTS) {
     // what lies behind the row's last step: zeros
-    float zero[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    const pair zero[4] = {};
     if (worker)
-      for (int k = first + busy * STEPS + es; k < last; k += STEPS) store_n<8>(y + (int64_t)k * a.py.step, zero, en, whole);
+      for (int k = first + busy * STEPS + es; k < last; k += STEPS)
+        store_pairs<8>((T*)a.y + (int64_t)k * a.py.step + (int64_t)b * a.py.row + d0 + ec, zero, en, whole);
     if (mine && a.s_out && seg == a.segments - 1) store_states(a.s_out + row, l, a.states, a.vec_s, s);
   } else if (mine) {
     store_states(a.ends + (int64_t)(seg + 1) * layer + place, l, NP, true, s);
@@ -274,25 +289,28 @@ __global__ void __launch_bounds__(NT1) scan_token(const ScanArgs a) {
   }
 }
 
+template <class T, int LANES, int PASS>
+bool launch_pass(const ScanArgs& a, int segments, cudaStream_t s) {
+  constexpr int bytes = Shape<T, LANES>::BYTES;
+  // per call: function attributes belong to the current device
+  if (bytes > 48 * 1024 && cudaFuncSetAttribute(scan_fwd<T, LANES, PASS>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
+  const dim3 grid((unsigned)(a.groups * a.blocks), (unsigned)a.batch, (unsigned)segments);
+  scan_fwd<T, LANES, PASS><<<grid, NT, bytes, counted(s)>>>(a);
+  return true;
+}
 template <class T, int LANES>
-void launch(const ScanArgs& a, cudaStream_t s) {
+bool launch(const ScanArgs& a, cudaStream_t s) {
   if (a.t == 1) {
     const dim3 grid((unsigned)((a.channels + NT1 / LANES - 1) / (NT1 / LANES)), (unsigned)a.batch);
     scan_token<T, LANES><<<grid, NT1, 0, counted(s)>>>(a);
-    return;
+    return true;
   }
-  dim3 grid((unsigned)(a.groups * a.blocks), (unsigned)a.batch, (unsigned)a.segments);
-  if (a.segments > 1) {
-    dim3 ends = grid;
-    --ends.z;                                         // nothing begins where the last one ends
-    scan_fwd<T, LANES, ENDS><<<ends, NT, 0, counted(s)>>>(a);
-  }
-  scan_fwd<T, LANES, OUTPUTS><<<grid, NT, 0, counted(s)>>>(a);
+  if (a.segments > 1 && !launch_pass<T, LANES, ENDS>(a, a.segments - 1, s)) return false;    // nothing begins where the last one ends
+  return launch_pass<T, LANES, OUTPUTS>(a, a.segments, s);
 }
 template <class T, int LANES>
-void launch_adj(const ScanArgs& a, cudaStream_t s) {
-  const dim3 grid((unsigned)(a.groups * a.blocks), (unsigned)a.batch, (unsigned)a.segments - 1);
-  scan_fwd<T, LANES, ADJOINTS><<<grid, NT, 0, counted(s)>>>(a);
+bool launch_adj(const ScanArgs& a, cudaStream_t s) {
+  return launch_pass<T, LANES, ADJOINTS>(a, a.segments - 1, s);
 }
 
 }  // namespace
@@ -306,11 +324,11 @@ int scan_fwd_channels(int lanes) { return NT / lanes; }
     case 4: return F<T, 4>(a, s);               \
     default: return F<T, 8>(a, s);              \
   }
-void scan_forward(const ScanArgs& a, bool half, cudaStream_t s) {
+bool scan_forward(const ScanArgs& a, bool half, cudaStream_t s) {
   if (half) { BY_LANES(launch, bf16) }
   BY_LANES(launch, float)
 }
-void scan_adjoints(const ScanArgs& a, bool half, cudaStream_t s) {
+bool scan_adjoints(const ScanArgs& a, bool half, cudaStream_t s) {
   if (half) { BY_LANES(launch_adj, bf16) }
   BY_LANES(launch_adj, float)
 }

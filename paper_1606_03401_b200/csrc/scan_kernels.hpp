@@ -10,11 +10,11 @@ namespace seq {
 
 int scan_fwd_channels(int lanes);       // channels of a block
 int scan_bwd_channels(int lanes);
-// Outputs and, with more than one segment, what they begin with.
-void scan_forward(const ScanArgs& a, bool half, cudaStream_t s);
+// Outputs and, with more than one segment, what they begin with.  False (here and below): a kernel's shared memory was refused.
+bool scan_forward(const ScanArgs& a, bool half, cudaStream_t s);
 // The adjoint that each segment hands to the one before it, for a gradient of zeros behind it (-> ends[segment + 1], dts).
-void scan_adjoints(const ScanArgs& a, bool half, cudaStream_t s);
-// Gradients: the walk backwards and the sums over blocks, rows and segments.  False: the kernel's shared memory was refused.
+bool scan_adjoints(const ScanArgs& a, bool half, cudaStream_t s);
+// Gradients: the walk backwards and the sums over blocks, rows and segments.
 bool scan_backward(const ScanArgs& a, bool half, float* dA, void* dB, void* dC, float* dskip, float* dbias, cudaStream_t s);
 
 }  // namespace seq
