@@ -6,6 +6,7 @@
 #include <cuda_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "launch.hpp"
 #include "mebptt.h"
@@ -18,10 +19,12 @@ namespace seq {
 namespace {
 
 constexpr int FWD = 4;        // channels of a thread: taps, inputs, and backward also gradients and sums, are held for each
-template <class T>
-constexpr int BWD = sizeof(T) == 2 ? 4 : 2;
+constexpr int bwd_channels(int bytes, int width) { return bytes == 2 && width <= 4 ? 4 : 2; }
+// Blocks an SM keeps: as many registers as that leaves a thread hold its channels without spilling.  (1000 x 64 x 1024 bfloat16, width 4:
+// 4 channels and 4 blocks 110 us, 2 channels and 5 blocks 135; float32, 32 rows: 2 and 5 83 us, 4 and 2 110.)
+constexpr int bwd_blocks(int bytes, int width) { return width > 4 ? 3 : bytes == 2 ? 4 : 5; }
 constexpr int U = 4;          // steps whose loads are issued together
-constexpr int ROWS = 8;       // runs of a block that share their channels
+constexpr int ROWS = 4;       // runs of a block that share their channels
 constexpr int COLS = 32;      // groups of channels of a block
 
 struct ConvArgs {
@@ -121,6 +124,7 @@ __global__ void __launch_bounds__(COLS* ROWS) conv_fwd(const ConvArgs a) {
 #pragma unroll
     for (int i = 0; i < U; ++i) raw[i] = next[i];
     load(k + U);
+    const bool full = k + U <= live;
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       pair v[P], p[P];
@@ -135,7 +139,7 @@ __global__ void __launch_bounds__(COLS* ROWS) conv_fwd(const ConvArgs a) {
         for (int j = 0; j + 1 < W - 1; ++j) win[j][c] = win[j + 1][c];
         if (W > 1) win[B - 1][c] = v[c];
       }
-      if (k + i < live) put<C, VEC>(y, p, nc);
+      if (full || k + i < live) put<C, VEC>(y, p, nc);
       y += a.py.step;
     }
   }
@@ -147,7 +151,7 @@ __global__ void __launch_bounds__(COLS* ROWS) conv_fwd(const ConvArgs a) {
 // dext_e = sum_j w[j] dp_{e - j} (+ ds_out where e >= n) over positions e = k + W - 1 of state and inputs together: the walk over k
 // emits position k, the input of step k - W + 1 (or the state's, for k < W - 1 in a row's first run).
 template <class T, int C, int W, bool VEC>
-__global__ void __launch_bounds__(COLS* ROWS, W <= 4 ? 2 : 1) conv_bwd(const ConvArgs a) {
+__global__ void __launch_bounds__(COLS* ROWS, bwd_blocks(sizeof(T), W)) conv_bwd(const ConvArgs a) {
   constexpr int P = C / 2, B = W > 1 ? W - 1 : 1;
   __shared__ float red[ROWS][COLS * C];
   const int group = blockIdx.y * COLS + threadIdx.x;
@@ -192,56 +196,66 @@ __global__ void __launch_bounds__(COLS* ROWS, W <= 4 ? 2 : 1) conv_bwd(const Con
 #pragma unroll
       for (int i = 0; i < U; ++i) { raw[i] = next[i]; rdy[i] = ndy[i]; }
       load(k + U);
+      // inside: the steps are the row's and this run's own, and the inputs that they emit are too
+      auto steps = [&](auto inside) {
+        constexpr bool IN = decltype(inside)::value;
 #pragma unroll
-      for (int i = 0; i < U; ++i) {
-        const int kk = k + i;
-        pair v[P], g[P], out[P];
-        unpack_pairs<C>(raw[i], v);
-        unpack_pairs<C>(rdy[i], g);
+        for (int i = 0; i < U; ++i) {
+          const int kk = k + i;
+          pair v[P], g[P], out[P];
+          unpack_pairs<C>(raw[i], v);
+          unpack_pairs<C>(rdy[i], g);
 #pragma unroll
-        for (int c = 0; c < P; ++c) {
-          if (a.silu) {
-            pair p = fma2(w[W - 1][c], v[c], bias[c]);
+          for (int c = 0; c < P; ++c) {
+            if (a.silu) {
+              pair p = fma2(w[W - 1][c], v[c], bias[c]);
 #pragma unroll
-            for (int j = 0; j < W - 1; ++j) p = fma2(w[j][c], win[j][c], p);
-            // silu' = s (1 + p (1 - s))
-            const pair s = sigmoid2(p), rest = fma2(s, both(-1.f), both(1.f));
-            g[c] = mul2(g[c], mul2(s, fma2(p, rest, both(1.f))));
+              for (int j = 0; j < W - 1; ++j) p = fma2(w[j][c], win[j][c], p);
+              // silu' = s (1 + p (1 - s))
+              const pair s = sigmoid2(p), rest = fma2(s, both(-1.f), both(1.f));
+              g[c] = mul2(g[c], mul2(s, fma2(p, rest, both(1.f))));
+            }
+            if (!IN && kk >= live) g[c] = 0;
+            if (IN || kk < k1) {
+              dw[W][c] = add2(dw[W][c], g[c]);
+              dw[W - 1][c] = fma2(g[c], v[c], dw[W - 1][c]);
+#pragma unroll
+              for (int j = 0; j < W - 1; ++j) dw[j][c] = fma2(g[c], win[j][c], dw[j][c]);
+            }
+#pragma unroll
+            for (int j = W - 1; j > 0; --j) dp[j][c] = dp[j - 1][c];
+            dp[0][c] = g[c];
+            out[c] = mul2(w[0][c], dp[0][c]);
+#pragma unroll
+            for (int j = 1; j < W; ++j) out[c] = fma2(w[j][c], dp[j][c], out[c]);
+#pragma unroll
+            for (int j = 0; j + 1 < W - 1; ++j) win[j][c] = win[j + 1][c];
+            if (W > 1) win[B - 1][c] = v[c];
           }
-          if (kk >= live) g[c] = 0;
-          if (kk < k1) {
-            dw[W][c] = add2(dw[W][c], g[c]);
-            dw[W - 1][c] = fma2(g[c], v[c], dw[W - 1][c]);
+          if constexpr (IN) {
+            put<C, VEC>(dx, out, nc);
+          } else if (kk < end) {
+            const int at = kk - (W - 1);             // the input that position kk belongs to; negative: the state's
+            if (W > 1 && a.ds_out && kk >= n && kk - n < W - 1) {
+              pair d[P];
+              unpack_pairs<C>(get<C, VEC>((const T*)a.ds_out + ((int64_t)b * (W - 1) + (kk - n)) * a.channels + c0, nc), d);
 #pragma unroll
-            for (int j = 0; j < W - 1; ++j) dw[j][c] = fma2(g[c], win[j][c], dw[j][c]);
+              for (int c = 0; c < P; ++c) out[c] = add2(out[c], d[c]);
+            }
+            if (at >= k0) {
+              if (at >= n)
+#pragma unroll
+                for (int c = 0; c < P; ++c) out[c] = 0;
+              put<C, VEC>(dx, out, nc);
+            } else if (W > 1 && at < 0 && a.ds_in) {
+              put<C, VEC>((T*)a.ds_in + ((int64_t)b * (W - 1) + kk) * a.channels + c0, out, nc);
+            }
           }
-#pragma unroll
-          for (int j = W - 1; j > 0; --j) dp[j][c] = dp[j - 1][c];
-          dp[0][c] = g[c];
-          out[c] = mul2(w[0][c], dp[0][c]);
-#pragma unroll
-          for (int j = 1; j < W; ++j) out[c] = fma2(w[j][c], dp[j][c], out[c]);
-#pragma unroll
-          for (int j = 0; j + 1 < W - 1; ++j) win[j][c] = win[j + 1][c];
-          if (W > 1) win[B - 1][c] = v[c];
+          dx += a.px.step;
         }
-        const int at = kk - (W - 1);               // the input that position kk belongs to; negative: the state's
-        if (W > 1 && a.ds_out && kk >= n && kk - n < W - 1 && kk < end) {
-          pair d[P];
-          unpack_pairs<C>(get<C, VEC>((const T*)a.ds_out + ((int64_t)b * (W - 1) + (kk - n)) * a.channels + c0, nc), d);
-#pragma unroll
-          for (int c = 0; c < P; ++c) out[c] = add2(out[c], d[c]);
-        }
-        if (kk < end && at >= k0) {
-          if (at >= n)
-#pragma unroll
-            for (int c = 0; c < P; ++c) out[c] = 0;
-          put<C, VEC>(dx, out, nc);
-        } else if (W > 1 && kk < end && at < 0 && a.ds_in) {
-          put<C, VEC>((T*)a.ds_in + ((int64_t)b * (W - 1) + kk) * a.channels + c0, out, nc);
-        }
-        dx += a.px.step;
-      }
+      };
+      if (k >= k0 + W - 1 && k + U <= min(k1, live)) steps(std::true_type{});
+      else steps(std::false_type{});
     }
   }
   // sums over the block's runs, one parameter after the other
@@ -268,8 +282,10 @@ __global__ void __launch_bounds__(256) conv_sums(const float* part, int parts, i
   __shared__ float red[8][32];
   const int64_t i = (int64_t)blockIdx.x * 32 + threadIdx.x, n = (int64_t)(width + 1) * D;
   float s = 0.f;
-  if (i < n)
+  if (i < n) {
+#pragma unroll 8
     for (int q = threadIdx.y; q < parts; q += 8) s += part[q * n + i];
+  }
   red[threadIdx.y][threadIdx.x] = s;
   __syncthreads();
   if (threadIdx.y != 0 || i >= n) return;
@@ -286,13 +302,14 @@ struct ConvPlan {
 };
 
 // Steps of a run: as many as leave every SM a thousand threads, 8 at least (a run begins with width - 1 inputs that its
-// neighbour also loads) and 32 at most (blocks of several waves even the SMs out).
+// neighbour also loads) and 32 at most, backward 64 (blocks of several waves even the SMs out).
 bool conv_plan(const mebptt_conv_desc* d, bool back, ConvPlan& p) {
-  const int C = p.C = !back ? FWD : d->dtype == MEBPTT_BF16 ? BWD<bf16> : BWD<float>;
+  const int C = p.C = back ? bwd_channels((int)elem_size(d->dtype), d->width) : FWD;
   p.groups = (d->channels + C - 1) / C;
   const int64_t threads = (int64_t)148 * 1024;
   int64_t run = (int64_t)p.groups * d->batch * d->t / threads;
-  run = run < 8 ? 8 : run > 32 ? 32 : run / 4 * 4;
+  const int64_t most = back ? 64 : 32;
+  run = run < 8 ? 8 : run > most ? most : run / 4 * 4;
   p.runs = (int)((d->t + run - 1) / run);
   p.run = (int)run;
   p.items = (int64_t)d->batch * p.runs;
@@ -313,7 +330,8 @@ template <class T, int W>
 void conv_launch(bool back, bool vec, const ConvPlan& p, const ConvArgs& a, cudaStream_t s) {
   const dim3 grid(p.blocks, p.cols), block(COLS, ROWS);
   (void)counted(s);
-  if (back) vec ? conv_bwd<T, BWD<T>, W, true><<<grid, block, 0, s>>>(a) : conv_bwd<T, BWD<T>, W, false><<<grid, block, 0, s>>>(a);
+  constexpr int CB = bwd_channels(sizeof(T), W);
+  if (back) vec ? conv_bwd<T, CB, W, true><<<grid, block, 0, s>>>(a) : conv_bwd<T, CB, W, false><<<grid, block, 0, s>>>(a);
   else vec ? conv_fwd<T, FWD, W, true><<<grid, block, 0, s>>>(a) : conv_fwd<T, FWD, W, false><<<grid, block, 0, s>>>(a);
 }
 template <class T>
