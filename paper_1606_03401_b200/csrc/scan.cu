@@ -47,8 +47,9 @@ bool check(const mebptt_scan_desc* d, ScanArgs& a, Cut& c) {
   c.np = 8 * lanes;
   c.blocks_f = (a.gchannels + chf - 1) / chf;
   c.blocks_b = (a.gchannels + chb - 1) / chb;
-  cut(d->t, (int64_t)d->groups * c.blocks_f * d->batch, SMS * 7, c.segment_f, c.segments_f);
-  cut(d->t, (int64_t)d->groups * c.blocks_b * d->batch, SMS * 4, c.segment_b, c.segments_b);
+  const bool half = d->dtype == MEBPTT_BF16;
+  cut(d->t, (int64_t)d->groups * c.blocks_f * d->batch, SMS * scan_fwd_blocks(lanes, half), c.segment_f, c.segments_f);
+  cut(d->t, (int64_t)d->groups * c.blocks_b * d->batch, SMS * scan_bwd_blocks(lanes, half, d->spacing), c.segment_b, c.segments_b);
   return true;
 }
 // What a grid can count.

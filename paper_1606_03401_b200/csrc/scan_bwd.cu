@@ -99,7 +99,9 @@ __device__ __forceinline__ void load_turned(const float* row, int l, int turn, i
   for (int i = 0; i < 4; ++i) s[i] = load_pair(row, PER_LANE * l + pair_at(i, turn), states, vec);
 }
 
-template <class T, int LANES, bool GATE>
+// VISITS: states are kept further apart than a tile is long.  (Without them the loop keeps its shape all the same: as straight code the
+// compiler would move so much of the backward half into the forward one that it spilt 276 bytes a thread, 1795 us instead of 1374.)
+template <class T, int LANES, bool GATE, bool VISITS>
 __global__ void __launch_bounds__(NT, 4) scan_bwd(const ScanArgs a) {
   using S = Shape<T, LANES>;
   using At = typename S::At;
@@ -172,8 +174,8 @@ __global__ void __launch_bounds__(NT, 4) scan_bwd(const ScanArgs a) {
     h.whole = a.vec_d && h.n == GW;
     return h;
   };
-  // Asks for the tile at k0, arrays into half `to`.  kept: and for the state before it.
-  auto fetch = [&](int k0, int to, bool kept) {
+  // Asks for the tile at k0, arrays into half `to`: for all of it, or for what a visit takes.  kept: and for the state before it.
+  auto fetch = [&](int k0, int to, bool kept, bool all) {
 #pragma unroll
     for (int q = 0; q < QG; ++q) {
       const Group h = group(q);
@@ -184,13 +186,15 @@ __global__ void __launch_bounds__(NT, 4) scan_bwd(const ScanArgs a) {
       };
       array(a.u, a.pu, 0);
       array(a.delta, a.pd, 1);
-      array(a.dy, a.py, 2);
-      if (GATE) array(a.z, a.pz, 3);
+      if (all) {
+        array(a.dy, a.py, 2);
+        if (GATE) array(a.z, a.pz, 3);
+      }
     }
 #pragma unroll
     for (int i = 0; i < QB; ++i) {
       const int q = tid + i * NT, n4 = (q % (NP / 4)) * 4, which = (q / (NP / 4)) & 1, k = k0 + q / (NP / 2);
-      if (q >= S::QUARTERS || k >= stop || n4 >= a.states) continue;
+      if (q >= S::QUARTERS || k >= stop || n4 >= a.states || (which && !all)) continue;
       fetch_n<4>(s_rows + q * E4, (which ? Cm + (int64_t)k * a.pc.step : Bm + (int64_t)k * a.pb.step) + n4, a.states - n4, a.vec_s && n4 + 4 <= a.states);
     }
     if (mine && kept) {
@@ -230,7 +234,7 @@ __global__ void __launch_bounds__(NT, 4) scan_bwd(const ScanArgs a) {
     f[0] = v.x; f[1] = v.y;
   };
   // the tile's planes and its B and C out of what was fetched
-  auto stage = [&](int k0, int half) {
+  auto stage = [&](int k0, int half, bool all) {
 #pragma unroll
     for (int p = 0; p < QG; ++p) {
       const Group h = group(p);
@@ -240,7 +244,7 @@ __global__ void __launch_bounds__(NT, 4) scan_bwd(const ScanArgs a) {
         pair bias[2];
         unpack_pairs<4>(array(half, 1, p), dt);
         unpack_pairs<4>(array(half, 0, p), x);
-        unpack_pairs<4>(array(half, 2, p), dv);
+        if (all) unpack_pairs<4>(array(half, 2, p), dv);
         channel_values(s_bias, h, bias);
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
@@ -248,7 +252,7 @@ __global__ void __launch_bounds__(NT, 4) scan_bwd(const ScanArgs a) {
           if (a.softplus) dt[j] = softplus2(dt[j]);
           x[j] = mul2(x[j], dt[j]);
         }
-        if (GATE) {
+        if (GATE && all) {
           pair z[2];
           unpack_pairs<4>(array(half, 3, p), z);
 #pragma unroll
@@ -257,12 +261,12 @@ __global__ void __launch_bounds__(NT, 4) scan_bwd(const ScanArgs a) {
       }
       to_plane(s_dt, h, dt);
       to_plane(s_x, h, x);
-      to_plane(s_dv, h, dv);
+      if (all) to_plane(s_dv, h, dv);
     }
 #pragma unroll
     for (int i = 0; i < QB; ++i) {
       const int q = tid + i * NT, n4 = (q % (NP / 4)) * 4, which = (q / (NP / 4)) & 1, step = q / (NP / 2);
-      if (q >= S::QUARTERS) continue;
+      if (q >= S::QUARTERS || (which && !all)) continue;
       float f[4] = {0, 0, 0, 0};
       if (k0 + step < stop && n4 < a.states) unpack<4>(fetched<T, 4>(s_rows + q * E4), f);
       const int upper = (n4 / 4) & 1, at_lane = n4 / PER_LANE;
@@ -299,9 +303,10 @@ __global__ void __launch_bounds__(NT, 4) scan_bwd(const ScanArgs a) {
   const int per = a.spacing / STEPS;
   int i = busy - 1, half = 0;                     // the tile to be worked on
   int visit = i >= 0 && i % per ? i - i % per : -1;   // the tile to be visited first, -1: none
-  if (i >= 0) fetch(first + (visit >= 0 ? visit : i) * STEPS, half, true);
+  if (i >= 0) fetch(first + (visit >= 0 ? visit : i) * STEPS, half, true, !VISITS || visit < 0);
   while (i >= 0) {
-    const int tile = visit >= 0 ? visit : i, k0 = first + tile * STEPS, steps = min(STEPS, stop - k0);
+    const bool visiting = visit >= 0;
+    const int tile = visiting ? visit : i, k0 = first + tile * STEPS, steps = min(STEPS, stop - k0);
     asm volatile("cp.async.wait_group 0;" ::: "memory");
     __syncthreads();                              // the tile before has been read
     pair state[STEPS + 1][4];                     // before a step
@@ -311,16 +316,16 @@ __global__ void __launch_bounds__(NT, 4) scan_bwd(const ScanArgs a) {
 #pragma unroll
       for (int q = 0; q < 4; ++q) state[0][q] = start(tile % per)[q];
     }
-    stage(k0, half);
-    int next = i, next_visit = visit;
-    if (visit < 0) {
+    stage(k0, half, !VISITS || !visiting);
+    int next = i, next_visit = -1;
+    if (!visiting) {
       --next;
-      next_visit = next >= 0 && next % per == per - 1 && per > 1 ? next - (per - 1) : -1;
-    } else if (++next_visit == i) {
-      next_visit = -1;
+      if (next >= 0 && next % per == per - 1 && per > 1) next_visit = next - (per - 1);
+    } else if (visit + 1 < i) {
+      next_visit = visit + 1;
     }
     const int next_tile = next_visit >= 0 ? next_visit : next;
-    if (next_tile >= 0) fetch(first + next_tile * STEPS, half ^ 1, next_tile % per == 0);
+    if (next_tile >= 0) fetch(first + next_tile * STEPS, half ^ 1, next_tile % per == 0, !VISITS || next_visit < 0);
     __syncthreads();
     // forwards
 #pragma unroll
@@ -338,7 +343,7 @@ __global__ void __launch_bounds__(NT, 4) scan_bwd(const ScanArgs a) {
       }
     }
     half ^= 1;
-    if (visit >= 0) {
+    if (visiting) {
 #pragma unroll
       for (int q = 0; q < 4; ++q) start(tile % per + 1)[q] = state[STEPS][q];
       visit = next_visit;
@@ -544,18 +549,19 @@ __global__ void __launch_bounds__(256) scan_sums(const Sums a) {
   else if (a.dbias) a.dbias[d] = v;
 }
 
-template <class T, int LANES, bool GATE>
-bool launch_gate(const ScanArgs& a, cudaStream_t s) {
-  const int bytes = Shape<T, LANES>::BYTES + (a.spacing > STEPS ? Shape<T, LANES>::STARTS : 0);
+template <class T, int LANES, bool GATE, bool VISITS>
+bool launch_kernel(const ScanArgs& a, cudaStream_t s) {
+  constexpr int bytes = Shape<T, LANES>::BYTES + (VISITS ? Shape<T, LANES>::STARTS : 0);
   // per call: function attributes belong to the current device
-  if (cudaFuncSetAttribute(scan_bwd<T, LANES, GATE>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
+  if (cudaFuncSetAttribute(scan_bwd<T, LANES, GATE, VISITS>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
   const dim3 grid((unsigned)(a.groups * a.blocks), (unsigned)a.batch, (unsigned)a.segments);
-  scan_bwd<T, LANES, GATE><<<grid, NT, bytes, counted(s)>>>(a);
+  scan_bwd<T, LANES, GATE, VISITS><<<grid, NT, bytes, counted(s)>>>(a);
   return true;
 }
 template <class T, int LANES>
 bool launch(const ScanArgs& a, cudaStream_t s) {
-  return a.z ? launch_gate<T, LANES, true>(a, s) : launch_gate<T, LANES, false>(a, s);
+  if (a.spacing > STEPS) return a.z ? launch_kernel<T, LANES, true, true>(a, s) : launch_kernel<T, LANES, false, true>(a, s);
+  return a.z ? launch_kernel<T, LANES, true, false>(a, s) : launch_kernel<T, LANES, false, false>(a, s);
 }
 template <class T>
 bool launch_lanes(const ScanArgs& a, cudaStream_t s) {
@@ -570,6 +576,21 @@ bool launch_lanes(const ScanArgs& a, cudaStream_t s) {
 }  // namespace
 
 int scan_bwd_channels(int lanes) { return NT / lanes; }
+
+template <class T>
+static int blocks_of_sm(int lanes, int spacing) {
+  auto room = [&](int bytes, int starts) {
+    const int n = 227 * 1024 / (bytes + (spacing > STEPS ? starts : 0) + 1024);
+    return n < 4 ? n : 4;
+  };
+  switch (lanes) {
+    case 1: return room(Shape<T, 1>::BYTES, Shape<T, 1>::STARTS);
+    case 2: return room(Shape<T, 2>::BYTES, Shape<T, 2>::STARTS);
+    case 4: return room(Shape<T, 4>::BYTES, Shape<T, 4>::STARTS);
+    default: return room(Shape<T, 8>::BYTES, Shape<T, 8>::STARTS);
+  }
+}
+int scan_bwd_blocks(int lanes, bool half, int spacing) { return half ? blocks_of_sm<bf16>(lanes, spacing) : blocks_of_sm<float>(lanes, spacing); }
 
 bool scan_backward(const ScanArgs& a, bool half, float* dA, void* dB, void* dC, float* dskip, float* dbias, cudaStream_t s) {
   if (!(half ? launch_lanes<bf16>(a, s) : launch_lanes<float>(a, s))) return false;

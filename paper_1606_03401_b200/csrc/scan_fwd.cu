@@ -317,6 +317,14 @@ bool launch_adj(const ScanArgs& a, cudaStream_t s) {
 
 int scan_fwd_channels(int lanes) { return NT / lanes; }
 
+template <class T>
+static int blocks_of_sm(int lanes) {
+  const int bytes = lanes == 1 ? Shape<T, 1>::BYTES : lanes == 2 ? Shape<T, 2>::BYTES : lanes == 4 ? Shape<T, 4>::BYTES : Shape<T, 8>::BYTES;
+  const int n = 227 * 1024 / (bytes + 1024);
+  return n < 7 ? n : 7;
+}
+int scan_fwd_blocks(int lanes, bool half) { return half ? blocks_of_sm<bf16>(lanes) : blocks_of_sm<float>(lanes); }
+
 #define BY_LANES(F, T)                          \
   switch (scan_lanes(a.states)) {               \
     case 1: return F<T, 1>(a, s);               \

@@ -10,6 +10,8 @@ namespace seq {
 
 int scan_fwd_channels(int lanes);       // channels of a block
 int scan_bwd_channels(int lanes);
+int scan_fwd_blocks(int lanes, bool half);      // blocks that an SM keeps at once
+int scan_bwd_blocks(int lanes, bool half, int spacing);
 // Outputs and, with more than one segment, what they begin with.  False (here and below): a kernel's shared memory was refused.
 bool scan_forward(const ScanArgs& a, bool half, cudaStream_t s);
 // The adjoint that each segment hands to the one before it, for a gradient of zeros behind it (-> ends[segment + 1], dts).
