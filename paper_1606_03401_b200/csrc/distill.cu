@@ -311,6 +311,7 @@ int finish(cudaError_t st, const DistillArgs& a, const mebptt_distill_desc* d, f
 }
 
 int run(const mebptt_distill_desc* d, DistillArgs& a, float* loss, cudaStream_t s) {
+  if (d->rows >= ((int64_t)1 << 31)) return MEBPTT_ERR_UNSUPPORTED;
   const size_t e = d->dtype == MEBPTT_BF16 ? 2 : 4;
   const int VE = (int)(16 / e);
   a.row = d->logits_row ? d->logits_row : d->vocabulary;

@@ -352,3 +352,80 @@ def test_captured_replayed_on_another_stream_and_bit_identical(make):
     graph.replay()
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(outputs(), want))
+
+
+def test_float32_storage_has_two_names():
+    a, b = Scan("fp32", 2, 40, 24, 16), Scan("fp32", 2, 40, 24, 16)
+    b.desc.dtype = B.MEBPTT_TF32
+    for p in (a, b):
+        p.forward()
+        p.backward()
+    assert all(torch.equal(x, y) for x, y in zip(a.outputs(), b.outputs()))
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("V", [60, 3000, 70001])
+def test_distill_gradient_at_another_alignment_than_the_logits(dtype, V):
+    p = Distill(dtype, 6, V, 9, pad=5, phase=1).upload()
+    p.row = V + 2
+    p.dmemory = torch.full((3 + 6 * p.row,), 977.0, device="cuda").to(p.X.dtype)
+    p.DX = p.dmemory.as_strided((6, V), (p.row, 1), 3)
+    p.desc.dlogits_row = p.row
+    p.both()
+    p.check()
+    p.DX.fill_(7.0)
+    p.apart()
+    p.check()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_distill_many_rows_of_every_kernel(dtype):
+    """More rows than there are warps, blocks or clusters at once, some of them without weight: rings go round, and clusters run
+    through rows in which they do not meet."""
+    for R, V in ((9000, 40), (1500, 3001), (330, 70000)):
+        p = Distill(dtype, R, V, 6, T=1.3, seed=R)
+        p.w[np.random.default_rng(0).random(R) < 0.4] = 0
+        p.w[R // 3:R // 3 + 40] = 0
+        p.upload()
+        p.both()
+        x = p.X.double() / float(np.float32(1.3))
+        logp = torch.log_softmax(x, 1)
+        q = torch.softmax(p.dev[1].double() / float(np.float32(1.3)), 1)
+        idx = p.dev[0].long()
+        w = p.dev[2].double()
+        row = w * 1.3 ** 2 * (q * (torch.log(q) - logp.gather(1, idx))).sum(1)
+        grad = (torch.exp(logp).scatter_add_(1, idx, -q) * (0.5 * p.scale * 1.3 * w)[:, None])
+        # sums of thousands of exponentials in 32 bits, each with some six roundings: 3e-6 of a row's largest term is plenty
+        assert torch.allclose(p.row_loss.double(), row, rtol=1e-5, atol=1e-5)
+        tol = 2 ** -8 if dtype == "bf16" else 1e-5
+        assert bool(((p.DX.double() - grad).abs() <= tol * grad.abs() + 3e-6 * grad.abs().amax(1, keepdim=True)).all())
+        assert torch.allclose(p.loss.double(), p.scale * row.sum(), rtol=1e-5)
+        first = [v.clone() for v in (p.loss, p.row_loss, p.DX)]
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            p.both()
+        p.DX.fill_(3.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(first, (p.loss, p.row_loss, p.DX)))
+
+
+def test_longer_sequences_and_more_rows_agree_with_shorter_calls():
+    """Two calls that hand a state on give what one call gives, in segments and without, with rows of every length."""
+    for N, t, D, S in ((1, 2100, 40, 16), (40, 90, 264, 16), (2, 700, 20, 30)):
+        p = Scan("fp32", N, t, D, S, ragged=N > 1, seed=t)
+        p.forward()
+        cut = t // 2 + 3
+        parts, s = [], p.dev["s_in"].clone()
+        for a, b in ((0, cut), (cut, t)):
+            L = None if p.lengths is None else torch.tensor(np.clip(p.lengths - a, 0, b - a), dtype=torch.int32, device="cuda")
+            u, delta, Bm, Cm, z = (x[a:b] for x in p._x("u", "delta", "Bm", "Cm", "z"))
+            d = B.make_scan_desc(N, D, S, 1, b - a, "fp32")
+            ws = torch.empty(B.mebptt_scan_workspace_bytes(d), dtype=torch.uint8, device="cuda")
+            y = torch.empty(b - a, N, D, device="cuda")
+            B.mebptt_scan_forward(d, u, delta, p.dev["A"], Bm, Cm, p.dev["skip"], z, p.dev["bias"], s, L, ws, _stream(), y, s)
+            parts.append(y)
+        y = torch.cat(parts)
+        # decays of up to t steps multiplied in another order: (4 + |x|) 2^-24 a step of what has not faded
+        scale = p.Lo["y"].x.abs().amax()
+        assert float((y - p.Lo["y"].x).abs().amax() / scale) < 2e-5 and torch.allclose(s, p.s_out, rtol=1e-4, atol=2e-5 * float(p.s_out.abs().max()))
