@@ -12,6 +12,7 @@
 #include "mebptt.h"
 #include "seq.hpp"
 #include "seq_dev.cuh"
+#include "sm100.cuh"
 
 namespace mebptt {
 namespace seq {
@@ -279,6 +280,7 @@ __global__ void __launch_bounds__(COLS* ROWS, bwd_blocks(sizeof(T), W)) conv_bwd
 
 // part [parts][width + 1][D] -> dw [D][width], dbias [D]; 8 threads share a column's sum.
 __global__ void __launch_bounds__(256) conv_sums(const float* part, int parts, int width, int D, float* dw, float* dbias) {
+  sm100::grid_dep_wait();
   __shared__ float red[8][32];
   const int64_t i = (int64_t)blockIdx.x * 32 + threadIdx.x, n = (int64_t)(width + 1) * D;
   float s = 0.f;
@@ -414,8 +416,9 @@ int mebptt_conv_backward(const mebptt_conv_desc* desc, const void* x, const void
   const int st = conv_run(desc, p, px, py, a, true, (cudaStream_t)stream);
   if (st != MEBPTT_OK) return st;
   const int64_t n = (int64_t)(desc->width + 1) * desc->channels;
-  conv_sums<<<(unsigned)((n + 31) / 32), dim3(32, 8), 0, counted((cudaStream_t)stream)>>>(a.part, (int)p.blocks, desc->width, desc->channels, dw, dbias);
-  return cudaGetLastError() == cudaSuccess ? MEBPTT_OK : MEBPTT_ERR_CUDA;
+  const cudaError_t e = launch_pdl(conv_sums, dim3((unsigned)((n + 31) / 32)), dim3(32, 8), 0, (cudaStream_t)stream, a.part, (int)p.blocks, desc->width,
+                                   desc->channels, dw, dbias);
+  return e == cudaSuccess ? MEBPTT_OK : MEBPTT_ERR_CUDA;
 }
 
 }  // extern "C"

@@ -20,6 +20,7 @@
 #include "mebptt.h"
 #include "seq.hpp"
 #include "seq_dev.cuh"
+#include "sm100.cuh"
 
 namespace cg = cooperative_groups;
 
@@ -276,6 +277,7 @@ __global__ void __launch_bounds__(MAX_THREADS) distill_kernel(const DistillArgs 
 
 // loss = scale sum of the rows' losses, one block, in a fixed order and in 64 bits
 __global__ void __launch_bounds__(1024) distill_total(const float* row_loss, int64_t rows, float scale, float* loss) {
+  sm100::grid_dep_wait();
   __shared__ double red[32];
   double s = 0.;
   for (int64_t i = threadIdx.x; i < rows; i += 1024) s += (double)row_loss[i];
@@ -306,8 +308,8 @@ cudaError_t launch(const DistillArgs& a, int64_t rows, int cluster, int threads,
 }
 
 int finish(cudaError_t st, const DistillArgs& a, const mebptt_distill_desc* d, float* loss, cudaStream_t s) {
-  if (st == cudaSuccess && loss) distill_total<<<1, 1024, 0, counted(s)>>>(a.row_loss, d->rows, d->scale, loss);
-  return cudaGetLastError() == cudaSuccess && st == cudaSuccess ? MEBPTT_OK : MEBPTT_ERR_CUDA;
+  if (st == cudaSuccess && loss) st = launch_pdl(distill_total, dim3(1), dim3(1024), 0, s, a.row_loss, d->rows, d->scale, loss);
+  return st == cudaSuccess ? MEBPTT_OK : MEBPTT_ERR_CUDA;
 }
 
 int run(const mebptt_distill_desc* d, DistillArgs& a, float* loss, cudaStream_t s) {

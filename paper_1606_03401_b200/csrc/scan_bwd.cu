@@ -24,6 +24,7 @@
 #include "scan.hpp"
 #include "scan_dev.cuh"
 #include "scan_kernels.hpp"
+#include "sm100.cuh"
 
 namespace mebptt {
 namespace seq {
@@ -106,6 +107,7 @@ __global__ void __launch_bounds__(NT, 4) scan_bwd(const ScanArgs a) {
   using S = Shape<T, LANES>;
   using At = typename S::At;
   constexpr int CH = S::CH, NP = S::NP, WARPS = S::WARPS, QG = S::QG, QB = S::QB, E4 = 4 * (int)sizeof(T);
+  sm100::grid_dep_wait();                         // for the kernel of the adjoints
   extern __shared__ __align__(16) uint8_t smem[];
   uint8_t* const s_arrays = smem;                                         // [2][u, delta, dy, z][groups][4]
   uint8_t* const s_rows = s_arrays + 8 * S::ARRAY;                        // [STEPS][B, C][NP], as in memory
@@ -181,14 +183,22 @@ __global__ void __launch_bounds__(NT, 4) scan_bwd(const ScanArgs a) {
       const Group h = group(q);
       if (!h.there || k0 + h.step >= stop) continue;
       uint8_t* const at = s_arrays + to * 4 * S::ARRAY + (tid + q * NT) * E4;
-      auto array = [&](const void* x, const Places& p, int which) {
-        fetch_n<4>(at + which * S::ARRAY, (const T*)x + (int64_t)(k0 + h.step) * p.step + (int64_t)b * p.row + d0 + h.c, h.n, h.whole);
-      };
-      array(a.u, a.pu, 0);
-      array(a.delta, a.pd, 1);
-      if (all) {
-        array(a.dy, a.py, 2);
-        if (GATE) array(a.z, a.pz, 3);
+      const int arrays = all ? GATE ? 4 : 3 : 2;
+      const void* const x[4] = {a.u, a.delta, a.dy, a.z};
+      const Places* const p[4] = {&a.pu, &a.pd, &a.py, &a.pz};
+      auto from = [&](int w) { return (const T*)x[w] + (int64_t)(k0 + h.step) * p[w]->step + (int64_t)b * p[w]->row + d0 + h.c; };
+      if (h.whole) {
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+          if (w < arrays) fetch_n<4>(at + w * S::ARRAY, from(w), GW, true);
+      } else {
+        Raw<T, 4> r[4];
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+          if (w < arrays) r[w] = load_raw<4>(from(w), h.n, false);
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+          if (w < arrays) memcpy(at + w * S::ARRAY, &r[w], sizeof r[w]);
       }
     }
 #pragma unroll
@@ -513,6 +523,7 @@ struct Sums {
 };
 template <class T>
 __global__ void __launch_bounds__(256) scan_sums(const Sums a) {
+  sm100::grid_dep_wait();
   __shared__ float red[8][32];
   const int tid = threadIdx.x;
   const int width = a.groups * 2 * a.np;
@@ -555,8 +566,7 @@ bool launch_kernel(const ScanArgs& a, cudaStream_t s) {
   // per call: function attributes belong to the current device
   if (cudaFuncSetAttribute(scan_bwd<T, LANES, GATE, VISITS>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
   const dim3 grid((unsigned)(a.groups * a.blocks), (unsigned)a.batch, (unsigned)a.segments);
-  scan_bwd<T, LANES, GATE, VISITS><<<grid, NT, bytes, counted(s)>>>(a);
-  return true;
+  return launch_on(a.segments > 1, scan_bwd<T, LANES, GATE, VISITS>, grid, dim3(NT), bytes, s, a) == cudaSuccess;
 }
 template <class T, int LANES>
 bool launch(const ScanArgs& a, cudaStream_t s) {
@@ -600,9 +610,7 @@ bool scan_backward(const ScanArgs& a, bool half, float* dA, void* dB, void* dC, 
   const int64_t bc = (int64_t)a.t * a.batch * a.groups * 2 * np, rest = (int64_t)a.channels * (a.states + 2);
   r.bc_blocks = (unsigned)((bc + 255) / 256);
   const unsigned grid = r.bc_blocks + (unsigned)((rest + 31) / 32);
-  if (half) scan_sums<bf16><<<grid, 256, 0, counted(s)>>>(r);
-  else scan_sums<float><<<grid, 256, 0, counted(s)>>>(r);
-  return true;
+  return (half ? launch_pdl(scan_sums<bf16>, dim3(grid), dim3(256), 0, s, r) : launch_pdl(scan_sums<float>, dim3(grid), dim3(256), 0, s, r)) == cudaSuccess;
 }
 
 }  // namespace seq

@@ -17,6 +17,7 @@
 #include "scan.hpp"
 #include "scan_dev.cuh"
 #include "scan_kernels.hpp"
+#include "sm100.cuh"
 
 namespace mebptt {
 namespace seq {
@@ -46,6 +47,7 @@ __global__ void __launch_bounds__(NT, 7) scan_fwd(const ScanArgs a) {
   using S = Shape<T, LANES>;
   using At = typename S::At;
   constexpr int CH = S::CH, STEPS = S::STEPS, NP = S::NP, QB = S::QB, E8 = 8 * (int)sizeof(T), E4 = 4 * (int)sizeof(T);
+  if (PASS == OUTPUTS) sm100::grid_dep_wait();         // for the kernel of the segments' ends
   extern __shared__ __align__(16) uint8_t smem[];
   float* const s_dt = reinterpret_cast<float*>(smem + 2 * S::RAW);    // dt, later the sums over states
   float* const s_x = s_dt + At::FLOATS;                // dt u; ADJOINTS: dy times the gate
@@ -295,8 +297,7 @@ bool launch_pass(const ScanArgs& a, int segments, cudaStream_t s) {
   // per call: function attributes belong to the current device
   if (bytes > 48 * 1024 && cudaFuncSetAttribute(scan_fwd<T, LANES, PASS>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
   const dim3 grid((unsigned)(a.groups * a.blocks), (unsigned)a.batch, (unsigned)segments);
-  scan_fwd<T, LANES, PASS><<<grid, NT, bytes, counted(s)>>>(a);
-  return true;
+  return launch_on(PASS == OUTPUTS && a.segments > 1, scan_fwd<T, LANES, PASS>, grid, dim3(NT), bytes, s, a) == cudaSuccess;
 }
 template <class T, int LANES>
 bool launch(const ScanArgs& a, cudaStream_t s) {
