@@ -107,13 +107,24 @@ __global__ void __launch_bounds__(NT, 7) scan_fwd(const ScanArgs a) {
   auto fetch = [&](int k0, int half) {
     uint8_t* const raw = smem + half * S::RAW;
     if (worker && k0 + es < stop) {
-      auto array = [&](const void* x, const Places& p, int which) {
-        fetch_n<8>(raw + which * S::ARRAY + tid * E8, (const T*)x + (int64_t)(k0 + es) * p.step + (int64_t)b * p.row + d0 + ec, en, whole);
-      };
-      array(a.delta, a.pd, 0);
-      if (PASS == ADJOINTS) array(a.dy, a.py, 1);
-      else array(a.u, a.pu, 1);
-      if (PASS != ENDS && a.z) array(a.z, a.pz, 2);
+      const bool gate = PASS != ENDS && a.z;
+      const void* const x[3] = {a.delta, PASS == ADJOINTS ? a.dy : a.u, a.z};
+      const Places* const p[3] = {&a.pd, PASS == ADJOINTS ? &a.py : &a.pu, &a.pz};
+      auto from = [&](int w) { return (const T*)x[w] + (int64_t)(k0 + es) * p[w]->step + (int64_t)b * p[w]->row + d0 + ec; };
+      uint8_t* const to = raw + tid * E8;
+      if (whole) {
+#pragma unroll
+        for (int w = 0; w < 3; ++w)
+          if (w < 2 || gate) fetch_n<8>(to + w * S::ARRAY, from(w), 8, true);
+      } else {
+        Raw<T, 8> r[3];
+#pragma unroll
+        for (int w = 0; w < 3; ++w)
+          if (w < 2 || gate) r[w] = load_raw<8>(from(w), en, false);
+#pragma unroll
+        for (int w = 0; w < 3; ++w)
+          if (w < 2 || gate) memcpy(to + w * S::ARRAY, &r[w], sizeof r[w]);
+      }
     }
 #pragma unroll
     for (int i = 0; i < QB; ++i) {
