@@ -784,7 +784,8 @@ cudaError_t launch(Kernel* kernel, const RingArgs& g, int64_t grid, int threads,
   cfg.attrs = at;
   cfg.numAttrs = g.cluster > 1 ? 1 : 0;
   // per call: function attributes belong to the current device
-  cudaError_t st = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  cudaError_t st = cudaSuccess;
+  if (smem > 48 * 1024) st = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (st != cudaSuccess) return st;
   if (g.cluster > 1) {
     const int64_t most = (int64_t)resident_clusters((const void*)kernel, cfg, g.cluster) * g.cluster;

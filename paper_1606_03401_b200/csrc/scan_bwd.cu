@@ -565,7 +565,7 @@ template <class T, int LANES, bool GATE, bool VISITS>
 bool launch_kernel(const ScanArgs& a, cudaStream_t s) {
   constexpr int bytes = Shape<T, LANES>::BYTES + (VISITS ? Shape<T, LANES>::STARTS : 0);
   // per call: function attributes belong to the current device
-  if (cudaFuncSetAttribute(scan_bwd<T, LANES, GATE, VISITS>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
+  if (bytes > 48 * 1024 && cudaFuncSetAttribute(scan_bwd<T, LANES, GATE, VISITS>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
   const dim3 grid((unsigned)(a.groups * a.blocks), (unsigned)a.batch, (unsigned)a.segments);
   return launch_on(a.segments > 1, scan_bwd<T, LANES, GATE, VISITS>, grid, dim3(NT), bytes, s, a) == cudaSuccess;
 }

@@ -124,7 +124,7 @@ def test_a_training_step_of_a_recurrent_language_model():
     got = m.backward(logits.clone(), saved)
     want_logits, loss, grads = m.reference()
     assert rel_l2(numpy(logits), want_logits.detach().numpy()) < TOL
-    assert abs(float(got["loss"]) - float(loss)) < TOL * float(loss)
+    assert abs(float(got["loss"]) - loss.item()) < TOL * loss.item()
     errs = {k: rel_l2(numpy(got[k]), g.numpy()) for k, g in grads.items()}
     assert set(errs) == {"x", "W_in", "W_out", "w", "bias", "A", "skip", "dbias"} and max(errs.values()) < TOL, errs
 

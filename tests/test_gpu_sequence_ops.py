@@ -178,6 +178,8 @@ class Scan:
     (2, 260, 24, 8, dict(spacing=32, layout="batch")),
     (3, 200, 12, 32, dict(spacing=16, G=2)),
     (3, 200, 9, 4, dict(state=False, gate=False)),
+    (2, 43, 256, 16, dict(G=2)),                                # groups of whole blocks, columns that load as one
+    (2, 90, 96, 12, dict(G=3, spacing=32, layout="sliced")),
 ])
 def test_scan_matches_the_oracle(dtype, N, t, D, S, kw):
     p = Scan(dtype, N, t, D, S, **kw)
@@ -429,3 +431,87 @@ def test_longer_sequences_and_more_rows_agree_with_shorter_calls():
         # decays of up to t steps multiplied in another order: (4 + |x|) 2^-24 a step of what has not faded
         scale = p.Lo["y"].x.abs().amax()
         assert float((y - p.Lo["y"].x).abs().amax() / scale) < 2e-5 and torch.allclose(s, p.s_out, rtol=1e-4, atol=2e-5 * float(p.s_out.abs().max()))
+
+
+def test_offsets_past_32_bits():
+    """Steps, rows and logits' rows that lie 2^31 elements apart, against the same data close together."""
+    far, t, N, D, S, W = 1 << 31, 3, 2, 24, 16, 4
+    c, p = Conv("bf16", N, t, D, W, ragged=False), Scan("bf16", N, t, D, S, ragged=False)
+    c.forward()
+    c.backward()
+    p.forward()
+    p.backward()
+    memory = torch.zeros((t - 1) * far + 4096, dtype=torch.bfloat16, device="cuda")
+    used = 0
+
+    def place(like=None, width=D):
+        nonlocal used
+        x = memory.as_strided((t, N, width), (far, 512, 1), used)
+        used += width
+        if like is not None:
+            x.copy_(like)
+        return x
+
+    at = (far, 512)
+    x, dy, y, dx = place(c.X.x), place(c.DY.x), place(), place()
+    desc = B.make_conv_desc(N, D, W, t, "bf16", True, at, at)
+    d, s_out, ds_in = c.dev, torch.empty_like(c.s_out), torch.empty_like(c.ds_in)
+    B.mebptt_conv_forward(desc, x, d["w"], d["bias"], d["s_in"], None, _stream(), y, s_out)
+    dw, db = torch.empty_like(c.dw), torch.empty_like(c.dbias)
+    B.mebptt_conv_backward(desc, x, d["w"], d["bias"], d["s_in"], None, dy, d["ds_out"], c.workspace, _stream(), dx, dw, db, ds_in)
+    for a, b in ((y, c.Y.x), (dx, c.DX.x), (s_out, c.s_out), (ds_in, c.ds_in), (dw, c.dw), (db, c.dbias)):
+        assert torch.equal(a, b)
+    memory.zero_()
+    used, d = 0, p.dev
+    u, delta, z, dy = (place(p.L[k].x) for k in ("u", "delta", "z", "dy"))
+    Bm, Cm = (place(p.L[k].x, S) for k in ("Bm", "Cm"))
+    y, du, dd, dz = (place() for _ in range(4))
+    dB, dC = place(width=S), place(width=S)
+    desc = B.make_scan_desc(N, D, S, 1, t, "bf16", True, 8, at, at, at, at, at, at)
+    s_out, dA, dk, db, ds_in = (torch.empty_like(v) for v in (p.s_out, p.dA, p.dskip, p.dbias, p.ds_in))
+    B.mebptt_scan_forward(desc, u, delta, d["A"], Bm, Cm, d["skip"], z, d["bias"], d["s_in"], None, p.workspace, _stream(), y, s_out, p.kept)
+    B.mebptt_scan_backward(desc, u, delta, d["A"], Bm, Cm, d["skip"], z, d["bias"], None, p.kept, dy, d["ds_out"], p.workspace, _stream(), du, dd, dA,
+                           dB, dC, dk, dz, db, ds_in)
+    for a, b in ((y, p.Lo["y"].x), (du, p.Lo["du"].x), (dd, p.Lo["ddelta"].x), (dz, p.Lo["dz"].x), (dB, p.Lo["dB"].x), (dC, p.Lo["dC"].x),
+                 (s_out, p.s_out), (dA, p.dA), (dk, p.dskip), (db, p.dbias), (ds_in, p.ds_in)):
+        assert torch.equal(a, b)
+    for V in (500, 3001):
+        q = Distill("bf16", 3, V, 7).upload()
+        q.both()
+        x = memory.as_strided((3, V), (far, 1), 1)
+        x.copy_(q.X)
+        desc = B.make_distill_desc(3, V, 7, "bf16", 1.0, q.scale, far, far)
+        row = torch.empty_like(q.row_loss)
+        B.mebptt_distill_loss_grad(desc, x, *q.dev, q.dloss, _stream(), None, row, x)
+        # (rows that begin elsewhere within 16 bytes sum in another order)
+        assert torch.allclose(row, q.row_loss, rtol=1e-5) and torch.allclose(x.float(), q.DX.float(), rtol=2 ** -7, atol=1e-7)
+
+
+def test_two_calls_at_once():
+    """Different problems on two streams, each with workspaces of its own, again and again."""
+    one = [Scan("bf16", 2, 500, 40, 16), Distill("bf16", 40, 70000, 9).upload(), Conv("bf16", 4, 60, 72, 4)]
+    two = [Scan("fp32", 3, 300, 24, 8, spacing=32, seed=5), Distill("fp32", 60, 9000, 30, seed=5).upload(), Conv("fp32", 3, 90, 40, 3, seed=5)]
+
+    def call(p):
+        if isinstance(p, Distill):
+            p.both()
+        else:
+            p.forward()
+            p.backward()
+
+    def outputs(p):
+        return [p.loss, p.row_loss, p.DX] if isinstance(p, Distill) else p.outputs()
+
+    for p in one + two:
+        call(p)
+    torch.cuda.synchronize()
+    want = [[v.clone() for v in outputs(p)] for p in one + two]
+    streams = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(10):
+        for a, b in zip(one, two):
+            for p, st in ((a, streams[0]), (b, streams[1])):
+                with torch.cuda.stream(st):
+                    call(p)
+    torch.cuda.synchronize()
+    for p, w in zip(one + two, want):
+        assert all(torch.equal(a, b) for a, b in zip(outputs(p), w))
