@@ -32,7 +32,7 @@ namespace {
 using namespace sm100;
 
 constexpr int PIECES = 8;               // 16-byte pieces of a thread: 64 bfloat16 or 32 float32 logits
-constexpr int MAX_CONSUMERS = 512, MAX_STAGES = 4;
+constexpr int MAX_HOLDING = 512, MAX_CONSUMERS = 928, MAX_STAGES = 4;   // threads that hold exponentials; threads of any block
 constexpr int AHEAD = 4;                // listed tokens of a lane that are loaded a row ahead
 constexpr int SMEM = 227 * 1024;
 
@@ -90,6 +90,17 @@ __device__ __forceinline__ float largest(const Raw<float, 4> (&r)[N]) {
   return fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
 }
 
+__device__ __forceinline__ float warp_max(float v) {
+#pragma unroll
+  for (int m = 16; m > 0; m /= 2) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, m));
+  return v;
+}
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+  for (int m = 16; m > 0; m /= 2) v += __shfl_xor_sync(0xffffffffu, v, m);
+  return v;
+}
+
 struct RingArgs {
   DistillArgs a;
   int cluster, stages, consumers, share;          // share: pieces of a block at most
@@ -109,8 +120,10 @@ struct Small {
   int failed;                                     // a wait has run out
 };
 
-template <class T, bool CLUSTER>
-__global__ void __launch_bounds__(MAX_CONSUMERS + 64, 1) distill_rows(const RingArgs g) {
+// LIGHT: exponentials are computed a second time for the gradient instead of being held, so that a block of up to 928 threads has
+// registers enough, and takes rows of twice the length.
+template <class T, bool CLUSTER, bool LIGHT>
+__global__ void __launch_bounds__((LIGHT ? MAX_CONSUMERS : MAX_HOLDING) + 64, 1) distill_rows(const RingArgs g) {
   constexpr int VE = 16 / (int)sizeof(T);
   extern __shared__ __align__(128) uint8_t sm[];
   const DistillArgs& a = g.a;
@@ -361,10 +374,20 @@ __global__ void __launch_bounds__(MAX_CONSUMERS + 64, 1) distill_rows(const Ring
       if (!mbar_wait(&o.full[s], (phases >> s) & 1)) o.failed = 1;      // bounded; a load of mapped memory always lands
       phases ^= 1u << s;
     }
-    pair e[PIECES][VE / 2];
+    Raw<T, VE> raw[PIECES];
+    pair e[LIGHT ? 1 : PIECES][VE / 2];
     float m = -INFINITY, sum = 0.f;
+    // exponentials of a piece, relative to m
+    auto exponentials = [&](const Raw<T, VE>& r, pair (&f)[VE / 2]) {
+      const pair from = both(m == -INFINITY ? 0.f : -m), k2 = both(k);
+      unpack_pairs<VE>(r, f);
+#pragma unroll
+      for (int j = 0; j < VE / 2; ++j) {
+        const float2 x = unpack2(mul2(add2(f[j], from), k2));
+        f[j] = pack2(ex2(x.x), ex2(x.y));
+      }
+    };
     if (live) {
-      Raw<T, VE> raw[PIECES];
 #pragma unroll
       for (int i = 0; i < PIECES; ++i) {
         const int p = tid + i * NC;
@@ -380,17 +403,15 @@ __global__ void __launch_bounds__(MAX_CONSUMERS + 64, 1) distill_rows(const Ring
         t_z[j] = at >= 0 ? to_f<T>(buf[at]) : 0.f;
       }
       m = largest(raw);
-      const pair from = both(m == -INFINITY ? 0.f : -m), k2 = both(k);
       pair sum_a = 0, sum_b = 0;
 #pragma unroll
       for (int i = 0; i < PIECES; ++i) {
-        unpack_pairs<VE>(raw[i], e[i]);
+        pair (&f)[VE / 2] = e[LIGHT ? 0 : i];
+        exponentials(raw[i], f);
 #pragma unroll
         for (int j = 0; j < VE / 2; ++j) {
-          const float2 x = unpack2(mul2(add2(e[i][j], from), k2));
-          e[i][j] = pack2(ex2(x.x), ex2(x.y));
-          if (j & 1) sum_a = add2(sum_a, e[i][j]);
-          else sum_b = add2(sum_b, e[i][j]);
+          if (j & 1) sum_a = add2(sum_a, f[j]);
+          else sum_b = add2(sum_b, f[j]);
         }
       }
       sum = sum2(add2(sum_a, sum_b));
@@ -405,14 +426,9 @@ __global__ void __launch_bounds__(MAX_CONSUMERS + 64, 1) distill_rows(const Ring
     consumers_sync(NC);
     float M = -INFINITY, S = 0.f;
     if (live) {
-      const int h = lane & 15;                    // each half of the warp has all of them
-      const float2 v = o.red[h < warps ? h : 0];
-      M = v.x;
-#pragma unroll
-      for (int q = 8; q > 0; q /= 2) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, q));
-      S = h >= warps ? 0.f : v.x == -INFINITY ? v.y : v.y * exp_over(v.x, M, k);
-#pragma unroll
-      for (int q = 8; q > 0; q /= 2) S += __shfl_xor_sync(0xffffffffu, S, q);
+      const float2 v = lane < warps ? o.red[lane] : make_float2(-INFINITY, 0.f);
+      M = warp_max(v.x);
+      S = warp_sum(v.x == -INFINITY ? v.y : v.y * exp_over(v.x, M, k));
     }
     if constexpr (CLUSTER) {
       if (meet) {
@@ -442,8 +458,11 @@ __global__ void __launch_bounds__(MAX_CONSUMERS + 64, 1) distill_rows(const Ring
         const int p = tid + i * NC;
         if (p < n) {
           pair f[VE / 2];
+          if constexpr (LIGHT) {
+            if (live) exponentials(raw[i], f);
+          }
 #pragma unroll
-          for (int j = 0; j < VE / 2; ++j) f[j] = live ? mul2(e[i][j], by) : 0;
+          for (int j = 0; j < VE / 2; ++j) f[j] = live ? mul2(LIGHT ? f[j] : e[LIGHT ? 0 : i][j], by) : 0;
           store_pairs<VE>(buf + p * VE, f, VE, true);
         }
       }
@@ -827,14 +846,16 @@ bool distill_ring(const DistillArgs& a, bool half, cudaStream_t s, cudaError_t& 
   // As few blocks to a row as hold it, and as many of them on an SM as fit: a meeting of a cluster costs a row some 0.7 us, and
   // blocks that wait for one another stand still together, while other rows' blocks do not.  (4096 rows of 32000 bfloat16 logits:
   // 105 us with one block a row, 118 with two, 148 with four.)
-  for (int cluster = 1; cluster <= 8; cluster *= 2) {
+  // Rows of up to twice what a block can hold as exponentials stay with one block all the same, which computes them twice.
+  for (int shape = 0; shape < 8; ++shape) {
+    const int cluster = 1 << (shape / 2), light = shape % 2;
     const int64_t share = (pieces + cluster - 1) / cluster;
-    if (share > MAX_CONSUMERS * PIECES) continue;
+    if (share > (light ? MAX_CONSUMERS : MAX_HOLDING) * PIECES) continue;
     g.cluster = cluster;
     g.share = (int)share;
     g.consumers = (int)((share + PIECES - 1) / PIECES + 31) / 32 * 32;
     const size_t small = small_bytes(g.share, VE, a.entries), stage = (size_t)share * 16;
-    int per_sm = 65536 / (96 * (g.consumers + 64));
+    int per_sm = 65536 / ((light ? 64 : 96) * (g.consumers + 64));
     if (per_sm > 6) per_sm = 6;
     while (per_sm > 1 && (size_t)per_sm * (small + 3 * stage + 1024) > SMEM) --per_sm;
     const size_t room = SMEM / per_sm - (per_sm > 1 ? 1024 : 0);
@@ -844,8 +865,11 @@ bool distill_ring(const DistillArgs& a, bool half, cudaStream_t s, cudaError_t& 
     int64_t clusters = (int64_t)sms * per_sm / cluster;
     if (clusters < 1) clusters = 1;
     if (clusters > a.rows) clusters = a.rows;
-    void (*const kernel)(const RingArgs) = half ? (cluster > 1 ? distill_rows<bf16, true> : distill_rows<bf16, false>)
-                                                : (cluster > 1 ? distill_rows<float, true> : distill_rows<float, false>);
+    void (*kernel)(const RingArgs);
+    if (light) kernel = half ? (cluster > 1 ? distill_rows<bf16, true, true> : distill_rows<bf16, false, true>)
+                             : (cluster > 1 ? distill_rows<float, true, true> : distill_rows<float, false, true>);
+    else kernel = half ? (cluster > 1 ? distill_rows<bf16, true, false> : distill_rows<bf16, false, false>)
+                       : (cluster > 1 ? distill_rows<float, true, false> : distill_rows<float, false, false>);
     st = launch(kernel, g, clusters * cluster, g.consumers + 64, small + (size_t)g.stages * stage, s);
     return true;
   }
