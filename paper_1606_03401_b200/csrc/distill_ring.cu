@@ -8,8 +8,8 @@
 // the listed tokens are put right there, and the stage is copied out.  One warp moves data, another prepares the next row's teacher
 // (softmax of the listed values, tokens listed twice) and adds up losses.  Row begins and ends that are not on 16-byte
 // boundaries go by plain loads and stores of the first one.
-// Measured, loss and gradient in bfloat16: 4096 rows of 32000 in 102 us (5.2 TB/s), 16384 of 8192 in 100 us, 512 of 128256 (clusters of
-// four) in 77 us (3.4 TB/s; a row's path of 4 us is longer than its bytes take).
+// Measured, loss and gradient in bfloat16: 4096 rows of 32000 in 102 us (5.2 TB/s), 16384 of 8192 in 100 us, 2048 of 50257 in 98 us
+// (4.2 TB/s), 512 of 128256 (clusters of four) in 72 us (3.6 TB/s; a row's path of 4 us is longer than its bytes take).
 //
 // Up to 2048 logits: a warp has a row and a ring to itself, so that nothing waits for another warp.  65536 rows of 1024: 100 us
 // (2.7 TB/s; instructions for the 64 listed tokens of each row are half of it).

@@ -53,7 +53,7 @@ constexpr int gemm_smem(int stages, int bn, int tps) { return stages * tps * (A_
 // TPS: tiles of 64 contraction indices per stage.  A grid of at most one wave has an SM for each tile of C, and one tile a
 // stage then passes at 60 to 100 GB/s an SM, however many stages there are: what takes the time is a stage's way
 // through its two barriers and the requests of its copies.  Three tiles a stage, requested together, come near what an
-// SM takes in (120 GB/s); us, one, two and three tiles a stage in 192 KB (narrow tiles of C: 120): 288 x 256, K = 3072
+// SM takes in (120 GB/s); us, one, two and three tiles a stage in 192 KB (narrow tiles of C: 120): 288 x 256, long K
 // 16.7, 12.0, 10.1; 128 x 8192, K = 2048 14.7, 12.1, 11.2; 4096 x 256, MN-major, K = 2048 17.4, 13.4, 12.5.  (Two
 // threads that request: no change.)  More tiles of C than SMs: one a stage, so that two CTAs share an SM and one's epilogue overlaps the other's products (2048 x 4096, K = 256: 13.4
 // against 20.7; 8192 x 8192, K = 4096: 489 against 629).

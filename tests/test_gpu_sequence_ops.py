@@ -515,3 +515,47 @@ def test_two_calls_at_once():
     torch.cuda.synchronize()
     for p, w in zip(one + two, want):
         assert all(torch.equal(a, b) for a, b in zip(outputs(p), w))
+
+
+@pytest.mark.parametrize("t", [1, 500, 3000])
+def test_a_state_that_does_not_fade_stays_as_it_is(t):
+    """A = 0: every decay is 1 exactly, however many steps, with and without segments; likewise steps of size 0."""
+    N, D, S = 2, 24, 16
+    r = np.random.default_rng(t)
+    s_in = device(r.standard_normal((N, D, S)))
+    zero = lambda *n: torch.zeros(*n, device="cuda")  # noqa: E731
+    delta, one = torch.rand(t, N, D, device="cuda"), torch.rand(t, N, S, device="cuda")
+    d = B.make_scan_desc(N, D, S, 1, t, "fp32", softplus=False)
+    ws = torch.empty(B.mebptt_scan_workspace_bytes(d), dtype=torch.uint8, device="cuda")
+    for step, A in ((delta, zero(D, S)), (zero(t, N, D), device(-np.exp(r.standard_normal((D, S)))))):
+        out = zero(N, D, S)
+        B.mebptt_scan_forward(d, zero(t, N, D), step, A, one, one, None, None, None, s_in, None, ws, _stream(), zero(t, N, D), out)
+        assert torch.equal(out, s_in)
+
+
+def test_lengths_outside_their_range_are_the_nearest_inside():
+    a, b = Scan("fp32", 4, 40, 24, 16, seed=3), Scan("fp32", 4, 40, 24, 16, seed=3)
+    c, e = Conv("fp32", 4, 40, 24, 4, seed=3), Conv("fp32", 4, 40, 24, 4, seed=3)
+    wild = torch.tensor([1 << 30, -5, 1, int(a.lengths[3])], dtype=torch.int32, device="cuda")
+    for p, q in ((a, b), (c, e)):
+        assert p.lengths[0] == 40 and p.lengths[1] == 0
+        q.dev["lengths"] = wild.clone()
+        q.dev["lengths"][2:] = p.dev["lengths"][2:]
+        for x in (p, q):
+            x.forward()
+            x.backward()
+        assert all(torch.equal(x, y) for x, y in zip(p.outputs(), q.outputs()))
+
+
+@pytest.mark.parametrize("V", [40, 5000, 40000])
+def test_distill_entries_that_are_not_there_may_hold_anything(V):
+    p = Distill("fp32", 5, V, 8)
+    p.i[:, 5:] = -1
+    p.upload()
+    p.both()
+    want = [v.clone() for v in (p.loss, p.row_loss, p.DX)]
+    p.dev[1][:, 5] = float("nan")
+    p.dev[1][:, 6] = float("inf")
+    p.dev[0][:, 7] = 1 << 30
+    p.both()
+    assert all(torch.equal(a, b) for a, b in zip(want, (p.loss, p.row_loss, p.DX)))
