@@ -11,16 +11,25 @@ using namespace mebptt::seq;
 
 namespace {
 
-// Steps of a segment and their number, for a kernel of `blocks` blocks a segment of which the device holds `room` at once.
-// Segments cost a kernel in front that walks the steps once more (backward: a lighter one), so that two of them gain little;
-// a segment has 32 steps at least, and there are 64 at most (each block folds what the others hand it).
-void cut(int64_t t, int64_t blocks, int64_t room, int& segment, int& segments) {
+// Steps of a segment and their number, for a kernel of `blocks` blocks a segment where `room` are wanted: as many as the device holds
+// at once, backward twice that.  Segments cost a kernel in front that walks the steps once more (backward: a lighter one, and more
+// sums to join), so that fewer than `least` of them lose by it; a segment begins where a state is kept and has 16 steps at least;
+// there are 64 at most (each block folds what the others hand it).
+// Measured in us, 512 steps of 1024 channels of 16 states in bf16, all kernels of the pass, with 1, 2, 3, 4 and 6 segments.
+// Forward: 32 rows (wanted 2) 157, 177, 187, 185, 195; 20 rows (wanted 3) 130, 137, 134, 126, 127; 16 rows (wanted 4) 109, 113, 116,
+// 103, 107; 10 rows (wanted 6) 108, 99, 87, 78, 79.
+// Backward: 32 rows (wanted 2) 420, 434, 451, 445, 440; 20 rows (wanted 3) 338, 342, 296, 300, 286; 16 rows (wanted 4) 269, 251, 246,
+// 238, 240; 10 rows (wanted 7) 265, 208, 178, 184, 166.
+// Backward with as many blocks as the device holds against twice that: 13 rows of 161 steps of 300 channels of 10 states in bf16
+// 49 and 43, but 4 rows of 2000 steps of 512 channels of 16 states in fp32 173 and 180.
+void cut(int64_t t, int64_t blocks, int64_t room, int least, int spacing, int& segment, int& segments) {
+  const int64_t unit = spacing > 16 ? spacing : 16;
   int64_t n = room / blocks;
-  if (n > t / TILE) n = t / TILE;
+  if (n > (t + unit - 1) / unit) n = (t + unit - 1) / unit;
   if (n > 64) n = 64;
-  if (n < 2) n = 1;
+  if (n < least) n = 1;
   int64_t len = (t + n - 1) / n;
-  len = (len + TILE - 1) / TILE * TILE;
+  len = (len + unit - 1) / unit * unit;
   segment = (int)len;
   segments = (int)((t + len - 1) / len);
 }
@@ -48,8 +57,8 @@ bool check(const mebptt_scan_desc* d, ScanArgs& a, Cut& c) {
   c.blocks_f = (a.gchannels + chf - 1) / chf;
   c.blocks_b = (a.gchannels + chb - 1) / chb;
   const bool half = d->dtype == MEBPTT_BF16;
-  cut(d->t, (int64_t)d->groups * c.blocks_f * d->batch, SMS * scan_fwd_blocks(lanes, half), c.segment_f, c.segments_f);
-  cut(d->t, (int64_t)d->groups * c.blocks_b * d->batch, SMS * scan_bwd_blocks(lanes, half, d->spacing), c.segment_b, c.segments_b);
+  cut(d->t, (int64_t)d->groups * c.blocks_f * d->batch, SMS * scan_fwd_blocks(lanes, half), 4, d->spacing, c.segment_f, c.segments_f);
+  cut(d->t, (int64_t)d->groups * c.blocks_b * d->batch, 2 * SMS * scan_bwd_blocks(lanes, half, d->spacing), 3, d->spacing, c.segment_b, c.segments_b);
   return true;
 }
 // What a grid can count.

@@ -10,7 +10,7 @@
 namespace mebptt {
 namespace seq {
 
-constexpr int TILE = 32;        // segments are multiples of it: of every tile, and of the widest spacing of kept states
+constexpr int TILE = 32;        // the widest spacing of kept states
 
 struct ScanArgs {
   const void* u; const void* delta; const void* z; const void* B; const void* C; const void* dy;

@@ -147,12 +147,20 @@ __global__ void __launch_bounds__(NT, 4) scan_bwd(const ScanArgs a) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) A[i] = mul2(A[i], both(kLog2e));
     if (a.ds_out) load_turned(a.ds_out + row, l, turn, a.states, a.vec_s, carry);
-    for (int j = a.segments - 1; j > seg; --j) {
-      pair e[4];
-      load_turned(a.ends + (j + 1) * layer + place, l, turn, NP, true, e);
-      const float dts = a.dts[((int64_t)j * a.batch + b) * a.channels + d];
+    for (int j0 = a.segments - 1; j0 > seg; j0 -= FOLD) {
+      pair e[FOLD][4];
+      float dts[FOLD];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) carry[i] = carry2(A[i], dts, carry[i], e[i]);
+      for (int j = 0; j < FOLD; ++j)
+        if (j0 - j > seg) {
+          load_turned(a.ends + (j0 - j + 1) * layer + place, l, turn, NP, true, e[j]);
+          dts[j] = a.dts[((int64_t)(j0 - j) * a.batch + b) * a.channels + d];
+        }
+#pragma unroll
+      for (int j = 0; j < FOLD; ++j)
+        if (j0 - j > seg)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) carry[i] = carry2(A[i], dts[j], carry[i], e[j][i]);
     }
   }
   for (int i = 0; i < PER_LANE; ++i) s_dA[tid * PER_LANE + i] = 0.f;

@@ -21,6 +21,7 @@ __device__ __forceinline__ pair decay2(pair dt, pair A) {
 }
 
 constexpr int PER_LANE = 8;     // states of a lane, as four pairs
+constexpr int FOLD = 4;         // segments whose ends are loaded together
 
 // Pair i of a lane's states lies here, from the first of them on.  `turn` exchanges pairs: bit 1 the halves of four states, bit 0 the
 // pairs of a half (lanes with other channels hold their states in another order, see sum_channels).

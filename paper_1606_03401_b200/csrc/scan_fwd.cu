@@ -82,12 +82,21 @@ __global__ void __launch_bounds__(NT, 7) scan_fwd(const ScanArgs a) {
   if (PASS == OUTPUTS && a.segments > 1) {
     if (mine) {
       load_states(a.ends + place, l, NP, true, s);
-      for (int j = 0; j < seg; ++j) {
-        pair e[4];
-        load_states(a.ends + (j + 1) * layer + place, l, NP, true, e);
-        const float dts = a.dts[((int64_t)j * a.batch + b) * a.channels + d];
+      // FOLD segments' loads at a time: one after the other they would cost a trip to the L2 each
+      for (int j0 = 0; j0 < seg; j0 += FOLD) {
+        pair e[FOLD][4];
+        float dts[FOLD];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[i] = carry2(A[i], dts, s[i], e[i]);
+        for (int j = 0; j < FOLD; ++j)
+          if (j0 + j < seg) {
+            load_states(a.ends + (j0 + j + 1) * layer + place, l, NP, true, e[j]);
+            dts[j] = a.dts[((int64_t)(j0 + j) * a.batch + b) * a.channels + d];
+          }
+#pragma unroll
+        for (int j = 0; j < FOLD; ++j)
+          if (j0 + j < seg)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[i] = carry2(A[i], dts[j], s[i], e[j][i]);
       }
     }
   } else if (PASS == OUTPUTS || (PASS == ENDS && seg == 0)) {
