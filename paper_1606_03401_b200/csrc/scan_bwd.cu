@@ -15,7 +15,7 @@
 // that keep the upper half hold it where the others hold the lower one.  So lanes hold their states in one of four orders
 // (`turn`), B and C lie in shared memory in all four, and the first two exchanges need no selections.
 //
-// Measured at 1000 steps x 64 rows x 1024 channels x 16 states in bfloat16, states kept every 8 steps: 1370 us; issue slots 56 %,
+// Measured at 1000 steps x 64 rows x 1024 channels x 16 states in bfloat16, states kept every 8 steps: 1350 us; issue slots 56 %,
 // shared-memory pipe 64 %, special functions 43 %: bound by the chains of a step (exponential, product, shuffles) at 16 warps an SM.
 #include <cuda_runtime.h>
 

@@ -6,12 +6,12 @@
 // share a channel, eight states each in registers, two to an instruction.  Per tile: the elementwise part (dt, dt u), eight channels
 // of a step to a thread; the scan out of shared memory; the gate, again elementwise.  Every thread fetches its part of the
 // next tile meanwhile, into shared memory, so that 72 registers are enough and an SM keeps seven blocks.
-// Measured at 1000 steps x 64 rows x 1024 channels x 16 states in bfloat16, states kept every 8 steps: 475 us; special functions
+// Measured at 1000 steps x 64 rows x 1024 channels x 16 states in bfloat16, states kept every 8 steps: 471 us; special functions
 // 61 % busy, shared-memory pipe 56 %, issue slots 57 %; 2.2 TB/s.
 //
 // Few rows and channels leave SMs without work, so long sequences are then cut into segments: a first kernel finds the state
 // that each segment ends in when it begins with zeros, and the sum of its dt, and the second one starts from those of the
-// segments before (s <- exp(A sum dt) s + end, one after the other).  4000 steps of one row of 2048 channels: 628 us without, 44 + 66
+// segments before (s <- exp(A sum dt) s + end, one after the other).  4000 steps of one row of 2048 channels: 628 us without, 44 + 68
 // with 32 segments.
 #include <cuda_runtime.h>
 

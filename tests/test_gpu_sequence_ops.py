@@ -188,6 +188,17 @@ def test_scan_matches_the_oracle(dtype, N, t, D, S, kw):
     p.check()
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("t,spacing", [(33, 8), (48, 8), (49, 16), (65, 8), (97, 32), (113, 16), (129, 32), (1024, 8)])
+def test_scan_in_every_number_of_segments(dtype, t, spacing):
+    """Three to sixty-four segments, whole batches of ends and rests of them, the last one of a single step; rows that end in the
+    first ones or before them."""
+    p = Scan(dtype, 5, t, 24, 16, spacing=spacing, ragged=True, seed=t)
+    p.forward()
+    p.backward()
+    p.check()
+
+
 def test_scan_without_kept_states_and_with_a_state_in_place():
     p = Scan("bf16", 3, 300, 24, 16, ragged=True)
     p.forward()
