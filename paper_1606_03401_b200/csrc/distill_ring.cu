@@ -802,9 +802,10 @@ cudaError_t launch(Kernel* kernel, const RingArgs& g, int64_t grid, int threads,
   at[0].val.clusterDim.x = (unsigned)g.cluster; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
   cfg.attrs = at;
   cfg.numAttrs = g.cluster > 1 ? 1 : 0;
-  // per call: function attributes belong to the current device
+  // Per call: function attributes belong to the current device.  Always the most that any shape takes: calls of other host threads, with
+  // rows of other lengths, set the same attribute of the same kernel between this and the launch.
   cudaError_t st = cudaSuccess;
-  if (smem > 48 * 1024) st = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (smem > 48 * 1024) st = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
   if (st != cudaSuccess) return st;
   if (g.cluster > 1) {
     const int64_t most = (int64_t)resident_clusters((const void*)kernel, cfg, g.cluster) * g.cluster;
