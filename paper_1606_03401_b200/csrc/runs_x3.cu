@@ -50,6 +50,7 @@ constexpr int PART_LD = 4 * RU + 4;      // row stride of the handed-over accumu
 constexpr int RECV_LD = RB + 4;          // row stride of a partial column of dh (floats)
 constexpr int SYNC_STRIDE = 32;          // words between the step counters of two groups
 constexpr int TMEM_COLS = 64;
+constexpr int MAX_KB = 16;               // tiles of 64 units in the widest layer (1024, x3_runs_supported)
 
 inline __host__ __device__ int whole_boxes(int KB) { return (KB + 3) / 4 * 4; }   // weights come in boxes of four tiles
 inline int fwd_smem(int KB) { return lone_smem((whole_boxes(KB) + RING * SLAB) * (int)TILE + 2 * RB * PART_LD * 4 + 1024); }
@@ -547,9 +548,9 @@ bool runs_begin(RunsX3& r, int I, int H, int B, const float* W, cudaStream_t s) 
   cudaMemsetAsync(r.exch_b, 0, (size_t)2 * r.groups * CS * 64 * HP * 2, s);
   cudaMemsetAsync(r.sync, 0, r.n_sync * 4, s);
   r.launches = 0;
-  const int KB = HP / 64;
-  cudaFuncSetAttribute(fwd_run_x3, cudaFuncAttributeMaxDynamicSharedMemorySize, fwd_smem(KB));
-  cudaFuncSetAttribute(bwd_run_x3, cudaFuncAttributeMaxDynamicSharedMemorySize, bwd_smem(KB));
+  // the most that any width takes: a step of another host thread sets the same limit between this and the launches
+  cudaFuncSetAttribute(fwd_run_x3, cudaFuncAttributeMaxDynamicSharedMemorySize, fwd_smem(MAX_KB));
+  cudaFuncSetAttribute(bwd_run_x3, cudaFuncAttributeMaxDynamicSharedMemorySize, bwd_smem(MAX_KB));
   return make_tmap_blocks64(&r.tm_h, r.exch_f, HP, (uint64_t)2 * r.groups * 64, (uint64_t)HP * 2, 64, SLAB) &&
          make_tmap_blocks64(&r.tm_w, r.w_f, HP, (uint64_t)H / RU * 64, (uint64_t)HP * 2, 64, 4) &&
          make_tmap_blocks64(&r.tm_dz, r.exch_b, HP, (uint64_t)2 * r.groups * CS * 64, (uint64_t)HP * 2, 64, SLAB) &&
