@@ -181,6 +181,7 @@ __global__ void __launch_bounds__(COLS* ROWS, bwd_blocks(sizeof(T), W)) conv_bwd
       for (int c = 0; c < P; ++c) dp[j][c] = 0;
 
     const int end = k1 + W - 1, live = min(end, n); // steps k1 .. end - 1 are the next run's: only their dp is needed
+    const int own = min(k1, n);                     // a step that the row does not have adds nothing, whatever lies before it
     const T* next_x = x + (int64_t)k0 * a.px.step;
     const T* next_dy = (const T*)a.dy + (int64_t)b * a.py.row + c0 + (int64_t)k0 * a.py.step;
     Raw<T, C> raw[U], rdy[U], next[U], ndy[U];
@@ -219,7 +220,7 @@ __global__ void __launch_bounds__(COLS* ROWS, bwd_blocks(sizeof(T), W)) conv_bwd
               g[c] = mul2(g[c], mul2(s, fma2(p, rest, both(1.f))));
             }
             if (!IN && kk >= live) g[c] = 0;
-            if (IN || kk < k1) {
+            if (IN || kk < own) {
               dw[W][c] = add2(dw[W][c], g[c]);
               dw[W - 1][c] = fma2(g[c], v[c], dw[W - 1][c]);
 #pragma unroll

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from paper_1606_03401_b200 import binding as B
-from tests.test_gpu_sequence_ops import Distill
+from tests.test_gpu_sequence_ops import Conv, Distill
 
 pytestmark = pytest.mark.gpu
 
@@ -59,3 +59,37 @@ def test_distill_calls_of_host_threads_whose_rows_differ_in_length(dtype, sizes)
     _together([lambda p=p: repeat(p) for p in problems])
     for p, w in zip(problems, want):
         assert all(torch.equal(x, y) for x, y in zip(outputs(p), w))
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("silu", [False, True])
+@pytest.mark.parametrize("W", [2, 4, 8])
+def test_conv_state_of_a_row_without_steps_is_handed_on_and_nothing_else(dtype, silu, W):
+    """Rows that a batch has no use for: their states may hold anything, the gradients of the taps know nothing of them."""
+    N, t, D = 5, 20, 40
+    a, b = (Conv(dtype, N, t, D, W, silu=silu, seed=W) for _ in range(2))
+    empty = [r for r in range(N) if a.lengths[r] == 0]
+    assert empty
+    for p, v in ((a, 0.0), (b, float("nan"))):
+        p.dev["s_in"][empty] = v
+        p.forward()
+        p.backward()
+    b.dev["s_in"][empty[0], :, ::2] = float("inf")
+    b.backward()
+    assert torch.equal(a.dw, b.dw) and torch.equal(a.dbias, b.dbias) and torch.equal(a.DX.x, b.DX.x) and torch.equal(a.ds_in, b.ds_in)
+    assert torch.equal(a.Y.x, b.Y.x) and bool(b.s_out[empty].isnan().all())
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_conv_last_input_reaches_only_the_taps_that_saw_it(dtype):
+    """The input of a row's last step was multiplied by the last tap alone, so that its value shows in that tap's gradient alone, where
+    the array goes on and where it ends."""
+    N, t, D, W = 3, 21, 24, 4
+    a, b = (Conv(dtype, N, t, D, W, silu=False, seed=9) for _ in range(2))
+    n = torch.tensor(a.lengths, device="cuda")
+    for p, v in ((a, 0.0), (b, float("inf"))):
+        for r in range(N):
+            if n[r] > 0:
+                p.X.x[int(n[r]) - 1, r] = v
+        p.backward()
+    assert torch.equal(a.dw[:, :W - 1], b.dw[:, :W - 1]) and not bool(b.dw[:, W - 1].isfinite().any())
