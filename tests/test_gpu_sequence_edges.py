@@ -1,11 +1,12 @@
 """GPU: the operators over sequences where calls meet: several host threads, rows and states at the edge of what counts, waits that run out."""
 import threading
 
+import numpy as np
 import pytest
 import torch
 
 from paper_1606_03401_b200 import binding as B
-from tests.test_gpu_sequence_ops import Conv, Distill
+from tests.test_gpu_sequence_ops import Conv, Distill, _stream
 
 pytestmark = pytest.mark.gpu
 
@@ -93,3 +94,35 @@ def test_conv_last_input_reaches_only_the_taps_that_saw_it(dtype):
                 p.X.x[int(n[r]) - 1, r] = v
         p.backward()
     assert torch.equal(a.dw[:, :W - 1], b.dw[:, :W - 1]) and not bool(b.dw[:, W - 1].isfinite().any())
+
+
+@pytest.mark.parametrize("first,rate", [(1e-30, 7.0), (1e30, -9.0), (-3e-20, 6.25), (2e-3, -8.0)])
+@pytest.mark.parametrize("t", [128, 700])
+def test_scan_states_that_grow_or_fade_by_more_than_the_range_of_the_type_within_a_segment(t, first, rate):
+    """Sixteen steps that multiply a state by e^100 and more, or by e^-128 and less, from a state small or large enough to stay a number
+    throughout.  All other steps leave the state as it is, and nothing is added to it.
+
+    Tolerance: the product e^(16 rate) is taken in one or two exponentials of the sum or in sixteen of the parts; sixteen parts are the
+    most, each (2 |rate| + 4) + 1 half steps of float32 (argument, function, product).  The last pair ends at 5e-59, below the type's
+    smallest normal number 2^-126, where results may be flushed to zero: off by less than that number."""
+    N, D, S = 2, 8, 16
+    zero = lambda *n: torch.zeros(*n, device="cuda")  # noqa: E731
+    delta = zero(t, N, D)
+    delta[64:80] = rate                                          # (whole segments: they begin at multiples of 16)
+    A, one = torch.ones(D, S, device="cuda"), torch.ones(t, N, S, device="cuda")
+    d = B.make_scan_desc(N, D, S, 1, t, "fp32", softplus=False)
+    ws = torch.empty(B.mebptt_scan_workspace_bytes(d, True), dtype=torch.uint8, device="cuda")
+    kept = torch.empty(B.mebptt_scan_kept_bytes(d), dtype=torch.uint8, device="cuda")
+    state, out, y, u = torch.full((N, D, S), first, device="cuda"), zero(N, D, S), zero(t, N, D), zero(t, N, D)
+    want = float(np.float32(first)) * np.exp(16 * rate)
+    tol = 16 * (2 * abs(rate) + 5) * 2.0 ** -24 * abs(want) + 2.0 ** -126
+    B.mebptt_scan_forward(d, u, delta, A, one, one, None, None, None, state, None, ws, _stream(), y, out, kept)
+    assert float((out.double() - want).abs().max()) <= tol
+    assert bool(y.isfinite().all()) and float((y[-1].double() - S * want).abs().max()) <= S * (tol + 4 * 2.0 ** -24 * abs(want))
+    # the same for what is handed back in time (from states of zeros, so that no other gradient is large)
+    B.mebptt_scan_forward(d, u, delta, A, one, one, None, None, None, None, None, ws, _stream(), y, out, kept)
+    du, dd, dA, dB, dC, back = zero(t, N, D), zero(t, N, D), zero(D, S), zero(t, N, S), zero(t, N, S), zero(N, D, S)
+    B.mebptt_scan_backward(d, u, delta, A, one, one, None, None, None, None, kept, zero(t, N, D), state, ws, _stream(), du, dd, dA, dB, dC, None, None,
+                           None, back)
+    assert float((back.double() - want).abs().max()) <= tol
+    assert not dA.any() and not dB.any() and not dC.any()
