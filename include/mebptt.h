@@ -502,8 +502,8 @@ int mebptt_gemm_bf16(const void *A, int64_t lda, int a_major, const void *B, int
  *   - Kernels only, on `stream` alone (a stream of the current device), with nothing allocated and
  *     nothing kept between calls: every call can be captured into a graph.  Calls whose work may
  *     overlap need workspaces of their own, two captured graphs too.
- *   - MEBPTT_ERR_UNSUPPORTED where a size passes what a grid can count (batch > 65535 for the scan,
- *     2^31 rows of logits).
+ *   - MEBPTT_ERR_UNSUPPORTED where a size passes what a grid or 32 bits can count (batch > 65535 or
+ *     2^24 groups of more than 32 states backward for the scan, 2^31 rows of logits).
  */
 
 /*

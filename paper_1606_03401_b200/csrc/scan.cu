@@ -61,9 +61,10 @@ bool check(const mebptt_scan_desc* d, ScanArgs& a, Cut& c) {
   cut(d->t, (int64_t)d->groups * c.blocks_b * d->batch, 2 * SMS * scan_bwd_blocks(lanes, half, d->spacing), 3, d->spacing, c.segment_b, c.segments_b);
   return true;
 }
-// What a grid can count.
-bool fits(const mebptt_scan_desc* d, const Cut& c) {
-  return d->batch <= 65535 && (double)d->t * d->batch * d->groups * 2 * c.np / 256 + (double)d->channels * (d->states + 2) / 32 < 2e9;
+// What a grid can count, and backward a row of sums over channels (both halves of every group's states) in 32 bits.
+bool fits(const mebptt_scan_desc* d, const Cut& c, bool back) {
+  return d->batch <= 65535 && (!back || (int64_t)d->groups * 2 * c.np <= INT32_MAX) &&
+         (double)d->t * d->batch * d->groups * 2 * c.np / 256 + (double)d->channels * (d->states + 2) / 32 < 2e9;
 }
 
 size_t up(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
@@ -154,7 +155,7 @@ int mebptt_scan_forward(const mebptt_scan_desc* desc, const void* u, const void*
   a.u = u; a.delta = delta; a.A = A; a.B = Bm; a.C = Cm; a.skip = skip; a.z = z; a.bias = delta_bias; a.s_in = s_in; a.lengths = lengths;
   a.y = y; a.s_out = s_out; a.kept = (float*)kept;
   if (!naturals(a, desc->dtype)) return MEBPTT_ERR_ARG;
-  if (!fits(desc, c)) return MEBPTT_ERR_UNSUPPORTED;
+  if (!fits(desc, c, false)) return MEBPTT_ERR_UNSUPPORTED;
   const Work w = work(desc, c, false);
   if (!workspace_fits(workspace, workspace_bytes, w.bytes)) return MEBPTT_ERR_WORKSPACE;
   a.ends = (float*)((char*)workspace + w.ends);
@@ -176,7 +177,7 @@ int mebptt_scan_backward(const mebptt_scan_desc* desc, const void* u, const void
   a.kept = (float*)kept; a.dy = dy; a.ds_out = ds_out; a.du = du; a.ddelta = ddelta; a.dz = dz; a.ds_in = ds_in;
   const size_t e = elem_size(desc->dtype);
   if (!naturals(a, desc->dtype) || !natural(dB, e) || !natural(dC, e) || !natural(dA, 4) || !natural(dskip, 4) || !natural(ddelta_bias, 4)) return MEBPTT_ERR_ARG;
-  if (!fits(desc, c)) return MEBPTT_ERR_UNSUPPORTED;
+  if (!fits(desc, c, true)) return MEBPTT_ERR_UNSUPPORTED;
   const Work w = work(desc, c, true);
   if (!workspace_fits(workspace, workspace_bytes, w.bytes)) return MEBPTT_ERR_WORKSPACE;
   char* const ws = (char*)workspace;

@@ -137,3 +137,10 @@ def test_tensors_of_another_type_or_place_are_refused():
     with pytest.raises(B.MebpttError) as e:
         B.mebptt_conv_forward(d, x, x, None, None, None, None, x, None)
     assert e.value.status == B.MEBPTT_ERR_ARG
+
+
+def test_scan_refuses_rows_of_sums_that_pass_32_bits():
+    wide = dict(batch=1, t=1, channels=1 << 24, groups=1 << 24)
+    for states in (33, 64):                                         # in memory 64 states a group, dB and dC: 2^31 values
+        assert _scan(True, states=states, **wide) == B.MEBPTT_ERR_UNSUPPORTED
+    assert _scan(True, states=64, nbytes=0, batch=1, t=1, channels=1 << 23, groups=1 << 23) == B.MEBPTT_ERR_WORKSPACE      # half as many: taken
