@@ -614,7 +614,7 @@ typedef struct {
   int32_t vocabulary, entries;
   int32_t dtype;
   int32_t reserved;            /* 0 */
-  float temperature, scale;    /* temperature > 0 */
+  float temperature, scale;    /* temperature > 0, its square a normal number (1.1e-19 to 1.8e19); scale finite */
   int64_t logits_row, dlogits_row;
 } mebptt_distill_desc;
 

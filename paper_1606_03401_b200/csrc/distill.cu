@@ -342,7 +342,10 @@ int run(const mebptt_distill_desc* d, DistillArgs& a, float* loss, cudaStream_t 
 
 bool check(const mebptt_distill_desc* d, const void* logits, const int32_t* indices, const float* values, const float* weights) {
   if (!d || d->rows < 1 || d->vocabulary < 1 || d->vocabulary > (1 << 30) || d->entries < 1 || d->entries > MAX_ENTRIES) return false;
-  if (!valid_dtype(d->dtype) || d->reserved || !(d->temperature > 0.f) || d->temperature > FLT_MAX || !(d->scale - d->scale == 0.f)) return false;
+  if (!valid_dtype(d->dtype) || d->reserved || !(d->scale - d->scale == 0.f)) return false;
+  // the losses carry the square: one that is infinite, or below the type's normal numbers, would make them so too
+  const float square = d->temperature * d->temperature;
+  if (!(d->temperature > 0.f) || !(square >= FLT_MIN) || square > FLT_MAX) return false;
   const int64_t most = (int64_t)1 << 40;
   if (d->rows > most || d->logits_row > most || d->dlogits_row > most) return false;
   if ((d->logits_row && d->logits_row < d->vocabulary) || (d->dlogits_row && d->dlogits_row < d->vocabulary)) return false;

@@ -144,3 +144,11 @@ def test_scan_refuses_rows_of_sums_that_pass_32_bits():
     for states in (33, 64):                                         # in memory 64 states a group, dB and dC: 2^31 values
         assert _scan(True, states=states, **wide) == B.MEBPTT_ERR_UNSUPPORTED
     assert _scan(True, states=64, nbytes=0, batch=1, t=1, channels=1 << 23, groups=1 << 23) == B.MEBPTT_ERR_WORKSPACE      # half as many: taken
+
+
+@pytest.mark.parametrize("which", ["loss", "grad", "both"])
+def test_distill_refuses_temperatures_whose_square_is_not_a_normal_number(which):
+    for T in (1e-45, 1e-40, 1e-30, 1.0e-19, 1.9e19, 1e30, 3e38):
+        assert _distill(which, temperature=T) == B.MEBPTT_ERR_ARG, T
+    for T in (1.1e-19, 1e-3, 1e4, 1.8e19):
+        assert _distill(which, temperature=T, rows=1 << 31) == B.MEBPTT_ERR_UNSUPPORTED, T        # taken, but for the rows
