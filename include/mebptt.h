@@ -606,8 +606,9 @@ int mebptt_scan_backward(const mebptt_scan_desc *desc, const void *u, const void
  *   mebptt_distill_grad       the gradient, from row_stats
  *   mebptt_distill_loss_grad  both, reading the logits once
  *
- * A device-side wait that runs out (each is bounded; none can while the device works) makes the losses
- * of the rows concerned NaN.
+ * A device-side wait that runs out (each is bounded; none can while the device works) makes NaN of what the
+ * waiting block had still to write of its rows: losses, statistics and its part of their gradients, in each of
+ * the three calls.  Rows that count nothing keep their zeros.
  */
 typedef struct {
   int64_t rows;
@@ -637,10 +638,12 @@ int mebptt_distill_loss_grad(const mebptt_distill_desc *desc, const void *logits
  * for one CTA more than exist, bit 1 does the same to the backward run kernels, bit 2 makes the
  * first pipeline stage of the batched contraction wait for 16 bytes more than its copies bring,
  * bit 3 does that to a phase of the kernel that walks a tape in pods, bit 4 makes the meeting of a
- * team of the other such kernel wait for one CTA more than it has;
+ * team of the other such kernel wait for one CTA more than it has; at the middle row (rows / 2), bit 5 makes the
+ * distillation loss wait for 16 bytes of logits more than its copies bring (the last block of a cluster), bit 6 its
+ * last block for the sums of one block more than share the row, bit 7 its first block for the losses of one more;
  * the waits concerned then give up after a few thousand polls.  No memory is touched that an
  * ordinary run would not touch.  mask = 0 restores normal behaviour; the setting is per process
- * and meant for single-threaded tests only.  Returns MEBPTT_ERR_ARG for a mask outside 0..31.
+ * and meant for single-threaded tests only.  Returns MEBPTT_ERR_ARG for a mask outside 0..255.
  */
 int mebptt_test_wait_fault(int mask);
 

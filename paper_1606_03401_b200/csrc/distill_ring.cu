@@ -8,6 +8,11 @@
 // the listed tokens are put right there, and the stage is copied out.  One warp moves data, another prepares the next row's teacher
 // (softmax of the listed values, tokens listed twice) and adds up losses.  Row begins and ends that are not on 16-byte
 // boundaries go by plain loads and stores of the first one.
+//
+// Every wait is bounded (none runs out while the device works).  After one that has run out a block, or a warp with a row to
+// itself, neither loads nor pushes nor waits for sums any more, since a barrier must not be armed a second time before its phase is over:
+// it leaves its rows from there on as lost (lost_row), waits once more, again bounded, for the loads that it has in flight, and ends.
+// The other blocks of its cluster get a sum that is not a number, or none and then run out of patience themselves.
 // Measured, loss and gradient in bfloat16: 4096 rows of 32000 in 102 us (5.2 TB/s), 16384 of 8192 in 100 us, 2048 of 50257 in 97 us
 // (4.2 TB/s), 512 of 128256 (clusters of four) in 72 us (3.6 TB/s; a row's path of 4 us is longer than its bytes take).
 //
@@ -23,6 +28,7 @@
 #include "seq.hpp"
 #include "seq_dev.cuh"
 #include "sm100.cuh"
+#include "tc.hpp"
 
 namespace mebptt {
 namespace seq {
@@ -56,12 +62,21 @@ __device__ __forceinline__ void push_pair(float2* at, uint64_t* bar, unsigned ra
                "r"(__float_as_uint(v.y)), "r"(bar_there)
                : "memory");
 }
-__device__ __forceinline__ bool wait_pushed(uint64_t* bar, uint32_t parity) {
-  for (uint32_t i = 0; i < kSpinLimit; ++i) {
+__device__ __forceinline__ bool wait_pushed(uint64_t* bar, uint32_t parity, uint32_t polls) {
+  for (uint32_t i = 0; i < polls; ++i) {
     if (mbar_try_wait_pushed(smem_u32(bar), parity)) return true;
     if (i > 64) __nanosleep(32);
   }
   return false;
+}
+// For a load, by a whole warp: all lanes learn the same.
+__device__ __forceinline__ bool wait_loaded(uint64_t* bar, uint32_t parity, uint32_t polls) {
+  bool there = false;
+  for (uint32_t i = 0; i < polls && !there; ++i) {
+    there = mbar_try_wait(bar, parity);
+    if (i > 64 && !there) __nanosleep(32);
+  }
+  return __all_sync(0xffffffffu, there);
 }
 __device__ __forceinline__ float exp_over(float x, float m, float k) { return ex2((x - m) * k); }
 
@@ -101,10 +116,38 @@ __device__ __forceinline__ float warp_sum(float v) {
   return v;
 }
 
+// Waits that a test lets run out (0: none), each at row `fault_row`.
+enum Fault { FAULT_LOAD = 1, FAULT_SUMS = 2, FAULT_LOSS = 4 };
+
 struct RingArgs {
   DistillArgs a;
   int cluster, stages, consumers, share;          // share: pieces of a block at most
+  int fault;
+  uint32_t polls;                                 // of a wait
+  int64_t fault_row;
+  __device__ bool faulty(int kind, int64_t row) const { return (fault & kind) && row == fault_row; }
 };
+
+// A row after a wait has run out, by a whole warp: loss, statistics (`tell`) and the gradient's elements from + first, from + first + by, ... below
+// `to` are no numbers, or what they always are where the row counts nothing.
+template <class T>
+__device__ __noinline__ void lost_row(const DistillArgs& a, int64_t r, int from, int to, int first, int by, bool tell) {
+  bool any = false;
+  for (int j = threadIdx.x % 32; j < a.entries; j += 32) {
+    const int idx = a.indices[r * a.entries + j];
+    any |= idx >= 0 && idx < a.vocabulary && a.values[r * a.entries + j] != -INFINITY;
+  }
+  const bool counts = __any_sync(0xffffffffu, any) && !(a.weights && a.weights[r] == 0.f);
+  const float v = counts ? NAN : 0.f;
+  if (a.gradient)
+    for (int i = from + first; i < to; i += by) ((T*)a.dlogits)[r * a.drow + i] = from_f<T>(v);
+  if (!tell) return;
+  if (a.row_loss) a.row_loss[r] = v;
+  if (a.row_stats) {
+    a.row_stats[2 * r] = v;
+    a.row_stats[2 * r + 1] = counts ? NAN : 1.f;
+  }
+}
 
 // Shared memory behind the stages.
 struct Small {
@@ -117,13 +160,13 @@ struct Small {
   float weight[MAX_STAGES];
   int any[2];                                     // a row has entries
   int counted[2];                                 // a row has them and a weight
-  int failed;                                     // a wait has run out
+  int64_t give_up;                                // the turn at which all warps leave their loops, a wait having run out in the one before
 };
 
 // LIGHT: exponentials are computed a second time for the gradient instead of being held, so that a block of up to 928 threads has
 // registers enough, and takes rows of twice the length.
 template <class T, bool CLUSTER, bool LIGHT>
-__global__ void __launch_bounds__((LIGHT ? MAX_CONSUMERS : MAX_HOLDING) + 64, 1) distill_rows(const RingArgs g) {
+__global__ void __launch_bounds__((LIGHT ? MAX_CONSUMERS : MAX_HOLDING) + 64, 1) distill_rows(const __grid_constant__ RingArgs g) {
   constexpr int VE = 16 / (int)sizeof(T);
   extern __shared__ __align__(128) uint8_t sm[];
   const DistillArgs& a = g.a;
@@ -171,24 +214,41 @@ __global__ void __launch_bounds__((LIGHT ? MAX_CONSUMERS : MAX_HOLDING) + 64, 1)
       mbar_init(&o.lost[s], 1);
     }
     mbar_fence_init();
-    o.failed = 0;
+    o.give_up = INT64_MAX;
   }
   for (int i = tid; i < words; i += blockDim.x) seen[i] = 0;
   __syncthreads();
   if constexpr (CLUSTER) cluster_sync();                                       // no block writes to another before it is there
 
+  // The end of every warp's way where a wait has run out in turn `from`: its share of that row and those behind it.
+  auto abandon = [&](int64_t from) {
+    for (int64_t it = from; it < rows; ++it) {
+      const Row w = row_at(it);
+      lost_row<T>(a, (int64_t)mine + it * clusters, max(w.p0 * VE - w.phase, 0), min(w.p1 * VE - w.phase, V), tid, blockDim.x, rank == 0 && tid == 0);
+    }
+    __syncwarp();
+    if constexpr (CLUSTER) {
+      cluster_sync();
+      for (int i = 0; i < 64; ++i) __nanosleep(1000);      // what others pushed here before they came has landed
+    }
+  };
+
   if (warp == warps) {
     // ---- the warp that moves data ----
+    uint32_t turns = 0, used = 0;                 // of a stage: loads so far are odd; there were any
     auto weight_of = [&](int64_t it) { return it < rows && a.weights ? a.weights[(int64_t)mine + it * clusters] : 1.f; };
     auto fetch = [&](int64_t it, int s, float weight) {
       if (it >= rows) return;
       if (lane == 0) o.weight[s] = weight;
       if (weight == 0.f) return;                  // not loaded, and not waited for
+      turns ^= 1u << s;
+      used |= 1u << s;
       const Row w = row_at(it);
       T* const buf = (T*)stage(s);
       if (lane == 0) {
         const uint32_t bytes = (uint32_t)(w.in1 - w.in0) * 16;
-        mbar_arrive_expect_tx(&o.full[s], bytes);
+        const bool faulty = g.faulty(FAULT_LOAD, (int64_t)mine + it * clusters) && (int)rank == g.cluster - 1;
+        mbar_arrive_expect_tx(&o.full[s], bytes + (faulty ? 16 : 0));
         if (bytes) bulk_in(buf + (w.in0 - w.p0) * VE, w.x + ((int64_t)w.in0 * VE - w.phase), bytes, &o.full[s]);
       }
       // what is not whole: elements before in0 and from in1 on
@@ -205,6 +265,14 @@ __global__ void __launch_bounds__((LIGHT ? MAX_CONSUMERS : MAX_HOLDING) + 64, 1)
     int last = NS - 1;                            // stage of row it - 1, and of row it - 1 + NS
     for (int64_t it = 0; it <= rows; ++it, last = last + 1 == NS ? 0 : last + 1) {
       __syncthreads();                            // row it - 1 is done with
+      if (o.give_up <= it) {
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+        __syncwarp();
+        for (int i = 0; i < NS; ++i)
+          if (used >> i & 1) wait_loaded(&o.full[i], ~turns >> i & 1, g.polls);
+        abandon(it - 1);
+        return;
+      }
       const float next = weight_of(it + NS);
       if (it >= 1 && a.gradient) {
         const Row w = row_at(it - 1);
@@ -313,17 +381,20 @@ __global__ void __launch_bounds__((LIGHT ? MAX_CONSUMERS : MAX_HOLDING) + 64, 1)
     for (int64_t it = 0; it <= rows; ++it) {
       __syncthreads();                            // row it has its teacher, row it - 1 its loss
       const int64_t was = it - 1;
+      if (o.give_up <= it) {
+        abandon(was);
+        return;
+      }
       if (was >= 0 && a.row_loss) {
         float v = lane < warps ? o.loss[was & 1][lane] : 0.f;
 #pragma unroll
         for (int m = 16; m > 0; m /= 2) v += __shfl_xor_sync(0xffffffffu, v, m);
-        if (o.failed) v = NAN;
         // (Blocks of a cluster meet in rows that count something only, once in each, to exchange their sums: none of them is
         // ever two such rows ahead of another, which is why two places for what they push are enough.)
         if (lane == 0) {
           due = CLUSTER && o.counted[was & 1];
           if (due) {
-            if (rank == 0) mbar_arrive_expect_tx(&o.lost[losses & 1], 8 * g.cluster);
+            if (rank == 0) mbar_arrive_expect_tx(&o.lost[losses & 1], 8 * (g.cluster + g.faulty(FAULT_LOSS, (int64_t)mine + was * clusters)));
             push_pair(&o.part[losses & 1][rank], &o.lost[losses & 1], 0, make_float2(v, 0.f));
           } else if (rank == 0) {
             a.row_loss[(int64_t)mine + was * clusters] = v;
@@ -335,7 +406,10 @@ __global__ void __launch_bounds__((LIGHT ? MAX_CONSUMERS : MAX_HOLDING) + 64, 1)
       if (due) {
         if (rank == 0) {
           float v = 0.f;
-          if (!wait_pushed(&o.lost[losses & 1], (losses >> 1) & 1)) v = NAN;
+          if (!wait_pushed(&o.lost[losses & 1], (losses >> 1) & 1, g.polls)) {
+            v = NAN;
+            o.give_up = it + 1;
+          }
           for (int c = 0; c < g.cluster; ++c) v += o.part[losses & 1][c].x;
           a.row_loss[(int64_t)mine + was * clusters] = v;
         }
@@ -355,6 +429,10 @@ __global__ void __launch_bounds__((LIGHT ? MAX_CONSUMERS : MAX_HOLDING) + 64, 1)
   int s = 0;
   for (int64_t it = 0; it <= rows; ++it, s = s + 1 == NS ? 0 : s + 1) {
     __syncthreads();
+    if (o.give_up <= it) {
+      abandon(it - 1);
+      return;
+    }
     if (it == rows) {
       if constexpr (CLUSTER) cluster_sync();
       break;
@@ -365,13 +443,15 @@ __global__ void __launch_bounds__((LIGHT ? MAX_CONSUMERS : MAX_HOLDING) + 64, 1)
     const bool meet = CLUSTER && live && !a.stats_in;
     if (tid == 0) {
       o.counted[it & 1] = live;
-      if (meet) mbar_arrive_expect_tx(&o.got[meetings & 1], 8 * g.cluster);
+      if (meet) mbar_arrive_expect_tx(&o.got[meetings & 1], 8 * (g.cluster + (g.faulty(FAULT_SUMS, (int64_t)mine + it * clusters) && (int)rank == g.cluster - 1)));
     }
     T* const buf = (T*)stage(s);
     const Row w = row_at(it);
     const int n = w.p1 - w.p0;
+    bool loaded = true;
     if (weight != 0.f) {
-      if (!mbar_wait(&o.full[s], (phases >> s) & 1)) o.failed = 1;      // bounded; a load of mapped memory always lands
+      loaded = wait_loaded(&o.full[s], (phases >> s) & 1, g.polls);
+      if (!loaded) o.give_up = it + 1;
       phases ^= 1u << s;
     }
     Raw<T, VE> raw[PIECES];
@@ -421,7 +501,7 @@ __global__ void __launch_bounds__((LIGHT ? MAX_CONSUMERS : MAX_HOLDING) + 64, 1)
       float v = m == -INFINITY ? sum : sum * exp_over(m, top, k);
 #pragma unroll
       for (int q = 16; q > 0; q /= 2) v += __shfl_xor_sync(0xffffffffu, v, q);
-      if (lane == 0) o.red[warp] = make_float2(top, v);
+      if (lane == 0) o.red[warp] = make_float2(top, loaded ? v : NAN);
     }
     consumers_sync(NC);
     float M = -INFINITY, S = 0.f;
@@ -434,7 +514,7 @@ __global__ void __launch_bounds__((LIGHT ? MAX_CONSUMERS : MAX_HOLDING) + 64, 1)
       if (meet) {
         if (tid < g.cluster) push_pair(&o.all[meetings & 1][rank], &o.got[meetings & 1], (unsigned)tid, make_float2(M, S));
         __syncwarp();
-        if (!wait_pushed(&o.got[meetings & 1], (meetings >> 1) & 1)) o.failed = 1;
+        if (!wait_pushed(&o.got[meetings & 1], (meetings >> 1) & 1, g.polls)) o.give_up = it + 1;
         M = -INFINITY;
         S = 0.f;
         for (int c = 0; c < g.cluster; ++c) M = fmaxf(M, o.all[meetings & 1][c].x);
@@ -506,7 +586,7 @@ __global__ void __launch_bounds__((LIGHT ? MAX_CONSUMERS : MAX_HOLDING) + 64, 1)
 // Short rows: a warp each, with a ring of its own, so that nothing waits for another warp.  `share` pieces a row at most.
 constexpr int WARPS = 4, ENTRIES = 128;
 template <class T, int PIECES>
-__global__ void __launch_bounds__(WARPS * 32, PIECES * 16 / (int)sizeof(T) == 32 ? 6 : 4) distill_warps(const RingArgs g) {
+__global__ void __launch_bounds__(WARPS * 32, PIECES * 16 / (int)sizeof(T) == 32 ? 6 : 4) distill_warps(const __grid_constant__ RingArgs g) {
   constexpr int VE = 16 / (int)sizeof(T), EPL = ENTRIES / 32;
   extern __shared__ __align__(128) uint8_t sm[];
   const DistillArgs& a = g.a;
@@ -547,7 +627,7 @@ __global__ void __launch_bounds__(WARPS * 32, PIECES * 16 / (int)sizeof(T) == 32
     T* const buf = (T*)(ring + s * stage_bytes);
     if (lane == 0) {
       const uint32_t bytes = (uint32_t)(w.in1 - w.in0) * 16;
-      mbar_arrive_expect_tx(&full[s], bytes);
+      mbar_arrive_expect_tx(&full[s], bytes + (g.faulty(FAULT_LOAD, r) ? 16 : 0));
       if (bytes) bulk_in(buf + w.in0 * VE, w.x + (w.in0 * VE - w.phase), bytes, &full[s]);
     }
     const int head = w.in0 * VE, tail = (w.pieces - w.in1) * VE;
@@ -579,7 +659,8 @@ __global__ void __launch_bounds__(WARPS * 32, PIECES * 16 / (int)sizeof(T) == 32
   look(first);
   uint32_t phases = 0;
   int s = 0;
-  for (int64_t r = first; r < a.rows; r += step, s = s + 1 == NS ? 0 : s + 1) {
+  int64_t r = first;
+  for (; r < a.rows; r += step, s = s + 1 == NS ? 0 : s + 1) {
     const float weight = weights[0];
     const Row w = row_at(r);
     T* const buf = (T*)(ring + s * stage_bytes);
@@ -597,9 +678,8 @@ __global__ void __launch_bounds__(WARPS * 32, PIECES * 16 / (int)sizeof(T) == 32
     const float next_w = weight_of(r + NS * step);
     look(r + step);
     const bool live = __any_sync(0xffffffffu, any) && weight != 0.f;
-    bool ok = true;
     if (weight != 0.f) {
-      ok = mbar_wait(&full[s], (phases >> s) & 1);       // bounded; a load of mapped memory always lands
+      if (!wait_loaded(&full[s], (phases >> s) & 1, g.polls)) break;
       phases ^= 1u << s;
     }
     // the stage of the row before: its gradient has been read out of it (that of this row is not yet on its way)
@@ -737,7 +817,7 @@ __global__ void __launch_bounds__(WARPS * 32, PIECES * 16 / (int)sizeof(T) == 32
         a.row_stats[2 * r + 1] = 1.f;
       }
     }
-    if (a.row_loss && lane == 0) a.row_loss[r] = ok ? loss : NAN;
+    if (a.row_loss && lane == 0) a.row_loss[r] = loss;
     if (a.gradient) {
       fence_proxy_async_shared();
       __syncwarp();
@@ -755,6 +835,14 @@ __global__ void __launch_bounds__(WARPS * 32, PIECES * 16 / (int)sizeof(T) == 32
     __syncwarp();
   }
   if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+  if (r < a.rows) {
+    // a wait has run out: the loads of this row and those ahead once more, then its rows from here on are lost
+    for (int i = 0; i < NS - 1; ++i) {
+      const int at = (s + i) % NS;
+      if (weight_of(r + i * step) != 0.f && r + i * step < a.rows) wait_loaded(&full[at], (phases >> at) & 1, g.polls);
+    }
+    for (; r < a.rows; r += step) lost_row<T>(a, r, 0, V, lane, 32, lane == 0);
+  }
 }
 
 size_t small_bytes(int share, int VE, int entries) {
@@ -839,6 +927,10 @@ bool distill_ring(const DistillArgs& a, bool half, cudaStream_t s, cudaError_t& 
   const int sms = sm_count();
   RingArgs g = {};
   g.a = a;
+  const int fault = tc::wait_fault_mask() >> 5;      // testing aid, 0 outside the tests of the bounded waits
+  g.fault = fault;
+  g.polls = fault ? tc::fault_poll_limit : kSpinLimit;
+  g.fault_row = a.rows / 2;
   if (pieces * VE <= 2048 && a.entries <= ENTRIES) {
     g.share = (int)pieces;
     st = half ? launch_warps<bf16>(g, sms, s) : launch_warps<float>(g, sms, s);

@@ -126,7 +126,8 @@ int64_t run_step(const Layout& y, const Plan* p, const StepPtrs& io, bool want_d
 // kernels waits for more than comes (one CTA, 16 pushed bytes, a piece of a ring that nobody writes); bit 1: likewise for the
 // backward run kernels; bit 2: the first stage of a GEMM expects 16 bytes more than its copies
 // bring; bit 3: a phase of a pod expects 16 bytes more than are pushed; bit 4: the meeting of a
-// team expects one arrival too many.  The waits then give up after `fault_poll_limit` polls instead of the usual limit, the
+// team expects one arrival too many; bits 5 to 7: the distillation loss, at one row, waits for 16 bytes of logits, one pair of sums, one part of
+// a loss more than come.  The waits then give up after `fault_poll_limit` polls instead of the usual limit, the
 // kernels leave through their ordinary exit path, and the status word receives MEBPTT_ERR_TIMEOUT.
 int short_runs_smem(bool backward, int H);   // dynamic shared memory of a CTA of the kernels for short runs of wide layers
 int wait_fault_mask();

@@ -126,3 +126,94 @@ def test_scan_states_that_grow_or_fade_by_more_than_the_range_of_the_type_within
                            None, back)
     assert float((back.double() - want).abs().max()) <= tol
     assert not dA.any() and not dB.any() and not dC.any()
+
+
+@pytest.fixture()
+def fault():
+    yield B.mebptt_test_wait_fault
+    B.mebptt_test_wait_fault(0)
+
+
+LOAD, SUMS, LOSS = 32, 64, 128
+KERNELS = [("bf16", 15000, 40, 1), ("fp32", 9000, 1500, 1), ("bf16", 4000, 5001, 1), ("fp32", 700, 28001, 1), ("fp32", 700, 29001, 2), ("bf16", 700, 50257, 1),
+           ("bf16", 500, 70000, 2), ("fp32", 300, 128256, 8)]     # type, rows, vocabulary, blocks of a row
+
+
+def _wide(dtype, R, V, seed=0):
+    """A problem made on the device (the oracle is not asked), every fifth row without weight, the middle one with."""
+    p = Distill(dtype, 1, 8, 8)
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    p.memory = p.X = torch.randn(R, V, device="cuda", generator=g).mul_(3).to(p.X.dtype)
+    p.dmemory = p.DX = torch.empty_like(p.X)
+    idx = torch.randint(0, V, (R, 8), device="cuda", generator=g).int()
+    weights = torch.rand(R, device="cuda", generator=g) + 0.1
+    weights[1::5] = 0
+    weights[R // 2] = 0.5
+    p.dev = (idx, torch.randn(R, 8, device="cuda", generator=g), weights)
+    p.desc = B.make_distill_desc(R, V, 8, dtype, 1.5, 1 / R)
+    p.row_loss, p.stats = (torch.empty(n * R, device="cuda") for n in (1, 2))
+    return p
+
+
+def _same(a, b):
+    return torch.equal(a.nan_to_num(nan=-1.0), b.nan_to_num(nan=-1.0)) and torch.equal(a.isnan(), b.isnan())
+
+
+@pytest.mark.parametrize("dtype,R,V,blocks,bit", [(*k, bit) for k in KERNELS for bit in (LOAD, SUMS, LOSS) if bit == LOAD or k[3] > 1])
+def test_distill_waits_that_run_out_show_in_every_output(fault, dtype, R, V, blocks, bit):
+    """The wait for the middle row's logits, the sums of its blocks or their parts of its loss expects more than ever comes and gives up.
+    From that row on the block writes no numbers; rows of others, those before and those without weight are what they are."""
+    p, row = _wide(dtype, R, V), R // 2
+    live = p.dev[2] != 0
+    p.both()
+    clean = [v.clone() for v in (p.loss, p.row_loss, p.DX)]
+    assert not any(bool(v.isnan().any()) for v in clean)
+
+    def check(lost, grad, whole):
+        """`lost`: the rows that show it; grad: the gradient; whole: from which of them on all of a row is lost, not one block's part alone."""
+        rows = lost.nonzero().flatten()
+        assert rows.numel() >= 2 and int(rows[0]) == row and bool(live[rows].all()) and rows.numel() < R // 4
+        assert torch.equal(grad[~lost], clean[2][~lost])
+        some = grad[rows].isnan()
+        assert bool(some[1:].any(1).all()) and bool(some[whole:].all())
+        return some[0]
+
+    fault(bit)
+    p.both()
+    torch.cuda.synchronize()                                        # returns: the waits give up, the kernel ends
+    fault(0)
+    lost = p.row_loss.isnan()
+    middle = check(lost, p.DX, 2 if bit == LOSS else 1)
+    assert bool(p.loss.isnan()) and torch.equal(p.row_loss[~lost], clean[1][~lost])
+    if bit == LOAD:
+        assert bool(middle.all())
+    else:                                                           # (the others' parts of the middle row are right)
+        assert bool(middle.any()) == (bit == SUMS) and not bool(middle.all())
+        assert torch.equal(p.DX[row][~middle], clean[2][row][~middle])
+    p.both()
+    assert all(torch.equal(a, b) for a, b in zip((p.loss, p.row_loss, p.DX), clean))
+
+    # the loss by itself: losses and statistics; the gradient by itself
+    B.mebptt_distill_loss(p.desc, p.X, *p.dev, _stream(), p.loss, p.row_loss, p.stats)
+    stats = p.stats.clone()
+    fault(bit)
+    B.mebptt_distill_loss(p.desc, p.X, *p.dev, _stream(), p.loss, p.row_loss, p.stats)
+    torch.cuda.synchronize()
+    lost, unknown = p.row_loss.isnan(), p.stats.view(R, 2).isnan()
+    assert torch.equal(lost.nonzero().flatten()[:1], torch.tensor([row], device="cuda")) and bool(p.loss.isnan())
+    assert torch.equal(p.stats.view(R, 2)[~lost], stats.view(R, 2)[~lost]) and torch.equal(p.row_loss[~lost], clean[1][~lost])
+    after = lost.nonzero().flatten()[1:]
+    assert after.numel() >= 1 and bool(unknown[after].all())
+    assert bool(unknown[row].any()) if bit == LOAD else torch.equal(p.stats.view(R, 2)[row], stats.view(R, 2)[row])
+    if bit == LOAD:
+        p.DX.fill_(7.0)
+        B.mebptt_distill_grad(p.desc, p.X, *p.dev, stats, p.dloss, _stream(), p.DX)
+        torch.cuda.synchronize()
+        middle = check(p.DX.isnan().any(1), p.DX, 1 if blocks == 1 else R)
+        assert bool(middle.all()) == (blocks == 1)
+    fault(0)
+    p.DX.fill_(7.0)
+    p.apart()
+    again = [v.clone() for v in (p.loss, p.row_loss, p.DX)]
+    p.apart()
+    assert all(_same(a, b) for a, b in zip(again, (p.loss, p.row_loss, p.DX))) and not bool(p.DX.isnan().any())
