@@ -9,15 +9,11 @@
 // (softmax of the listed values, tokens listed twice) and adds up losses.  Row begins and ends that are not on 16-byte
 // boundaries go by plain loads and stores of the first one.
 //
-// Every wait is bounded (none runs out while the device works).  After one that has run out a block, or a warp with a row to
-// itself, neither loads nor pushes nor waits for sums any more, since a barrier must not be armed a second time before its phase is over:
-// it leaves its rows from there on as lost (lost_row), waits once more, again bounded, for the loads that it has in flight, and ends.
-// The other blocks of its cluster get a sum that is not a number, or none and then run out of patience themselves.
-// Measured, loss and gradient in bfloat16: 4096 rows of 32000 in 102 us (5.2 TB/s), 16384 of 8192 in 100 us, 2048 of 50257 in 97 us
-// (4.2 TB/s), 512 of 128256 (clusters of four) in 72 us (3.6 TB/s; a row's path of 4 us is longer than its bytes take).
-//
-// Up to 2048 logits: a warp has a row and a ring to itself, so that nothing waits for another warp.  65536 rows of 1024: 100 us
-// (2.7 TB/s; instructions for the 64 listed tokens of each row are half of it).
+// Every wait is bounded (none runs out while the device works).  A block in which one has run out loads no more rows, since a barrier
+// must not be armed a second time before its phase is over, and neither pushes nor waits for what the cluster exchanges there:
+// the other blocks get a sum that is not a number, or none and then run out of patience themselves.  Its rows from that one on are
+// lost: its warp that moves data writes them as no numbers (lost_row) and waits at the end, once more bounded, for the loads in
+// flight.  (All warps go through all turns: a way out of the loop costs the warps that compute 6 % at 4096 rows of 32000.)
 #include <cuda_runtime.h>
 
 #include <cstdint>
@@ -160,7 +156,7 @@ struct Small {
   float weight[MAX_STAGES];
   int any[2];                                     // a row has entries
   int counted[2];                                 // a row has them and a weight
-  int64_t give_up;                                // the turn at which all warps leave their loops, a wait having run out in the one before
+  int64_t lost_from;                              // the first row that is lost, counted as the block takes them (none: INT64_MAX)
 };
 
 // LIGHT: exponentials are computed a second time for the gradient instead of being held, so that a block of up to 928 threads has
@@ -214,23 +210,15 @@ __global__ void __launch_bounds__((LIGHT ? MAX_CONSUMERS : MAX_HOLDING) + 64, 1)
       mbar_init(&o.lost[s], 1);
     }
     mbar_fence_init();
-    o.give_up = INT64_MAX;
+    o.lost_from = INT64_MAX;
   }
   for (int i = tid; i < words; i += blockDim.x) seen[i] = 0;
   __syncthreads();
   if constexpr (CLUSTER) cluster_sync();                                       // no block writes to another before it is there
 
-  // The end of every warp's way where a wait has run out in turn `from`: its share of that row and those behind it.
-  auto abandon = [&](int64_t from) {
-    for (int64_t it = from; it < rows; ++it) {
-      const Row w = row_at(it);
-      lost_row<T>(a, (int64_t)mine + it * clusters, max(w.p0 * VE - w.phase, 0), min(w.p1 * VE - w.phase, V), tid, blockDim.x, rank == 0 && tid == 0);
-    }
-    __syncwarp();
-    if constexpr (CLUSTER) {
-      cluster_sync();
-      for (int i = 0; i < 64; ++i) __nanosleep(1000);      // what others pushed here before they came has landed
-    }
+  // (Set in the turn of that row, by whoever finds out, and read in later ones.)
+  auto lose = [&](int64_t it) {
+    if (it < o.lost_from) o.lost_from = it;
   };
 
   if (warp == warps) {
@@ -265,16 +253,12 @@ __global__ void __launch_bounds__((LIGHT ? MAX_CONSUMERS : MAX_HOLDING) + 64, 1)
     int last = NS - 1;                            // stage of row it - 1, and of row it - 1 + NS
     for (int64_t it = 0; it <= rows; ++it, last = last + 1 == NS ? 0 : last + 1) {
       __syncthreads();                            // row it - 1 is done with
-      if (o.give_up <= it) {
-        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
-        __syncwarp();
-        for (int i = 0; i < NS; ++i)
-          if (used >> i & 1) wait_loaded(&o.full[i], ~turns >> i & 1, g.polls);
-        abandon(it - 1);
-        return;
-      }
+      const bool lost = o.lost_from < it;
       const float next = weight_of(it + NS);
-      if (it >= 1 && a.gradient) {
+      if (lost) {
+        const Row w = row_at(it - 1);
+        lost_row<T>(a, (int64_t)mine + (it - 1) * clusters, max(w.p0 * VE - w.phase, 0), min(w.p1 * VE - w.phase, V), lane, 32, rank == 0 && lane == 0);
+      } else if (it >= 1 && a.gradient) {
         const Row w = row_at(it - 1);
         const T* const buf = (const T*)stage(last);
         if (lane == 0) {
@@ -290,12 +274,20 @@ __global__ void __launch_bounds__((LIGHT ? MAX_CONSUMERS : MAX_HOLDING) + 64, 1)
         if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
         __syncwarp();
       }
-      if (it < rows) fetch(it - 1 + NS, last, weight);
+      if (it < rows) fetch(it - 1 + NS, last, lost ? 0.f : weight);
       weight = next;
     }
     if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     __syncwarp();
-    if constexpr (CLUSTER) cluster_sync();        // no block leaves while another pushes to it
+    const bool lost = o.lost_from != INT64_MAX;
+    if (lost)
+      for (int i = 0; i < NS; ++i)
+        if (used >> i & 1) wait_loaded(&o.full[i], ~turns >> i & 1, g.polls);
+    if constexpr (CLUSTER) {
+      cluster_sync();                             // no block leaves while another pushes to it
+      if (lost)
+        for (int i = 0; i < 64; ++i) __nanosleep(1000);      // what was pushed and not waited for has landed
+    }
     return;
   }
   if (warp == warps + 1) {
@@ -381,11 +373,7 @@ __global__ void __launch_bounds__((LIGHT ? MAX_CONSUMERS : MAX_HOLDING) + 64, 1)
     for (int64_t it = 0; it <= rows; ++it) {
       __syncthreads();                            // row it has its teacher, row it - 1 its loss
       const int64_t was = it - 1;
-      if (o.give_up <= it) {
-        abandon(was);
-        return;
-      }
-      if (was >= 0 && a.row_loss) {
+      if (was >= 0 && a.row_loss && was < o.lost_from) {
         float v = lane < warps ? o.loss[was & 1][lane] : 0.f;
 #pragma unroll
         for (int m = 16; m > 0; m /= 2) v += __shfl_xor_sync(0xffffffffu, v, m);
@@ -408,7 +396,7 @@ __global__ void __launch_bounds__((LIGHT ? MAX_CONSUMERS : MAX_HOLDING) + 64, 1)
           float v = 0.f;
           if (!wait_pushed(&o.lost[losses & 1], (losses >> 1) & 1, g.polls)) {
             v = NAN;
-            o.give_up = it + 1;
+            lose(it);
           }
           for (int c = 0; c < g.cluster; ++c) v += o.part[losses & 1][c].x;
           a.row_loss[(int64_t)mine + was * clusters] = v;
@@ -425,14 +413,11 @@ __global__ void __launch_bounds__((LIGHT ? MAX_CONSUMERS : MAX_HOLDING) + 64, 1)
   // ---- the warps that compute ----
   uint32_t phases = 0;                            // of the stages' barriers: a stage that was not loaded keeps its own
   uint32_t meetings = 0;                          // of the cluster's blocks
+  bool alone = false;                             // one of them has not come about
   const float dscale = (a.gradient && a.dloss ? *a.dloss : 1.f) * a.scale * a.T;
   int s = 0;
   for (int64_t it = 0; it <= rows; ++it, s = s + 1 == NS ? 0 : s + 1) {
     __syncthreads();
-    if (o.give_up <= it) {
-      abandon(it - 1);
-      return;
-    }
     if (it == rows) {
       if constexpr (CLUSTER) cluster_sync();
       break;
@@ -440,7 +425,7 @@ __global__ void __launch_bounds__((LIGHT ? MAX_CONSUMERS : MAX_HOLDING) + 64, 1)
     const int slot = (int)(it & 1) * K;
     const float weight = o.weight[s];
     const bool live = weight != 0.f && o.any[it & 1];
-    const bool meet = CLUSTER && live && !a.stats_in;
+    const bool meet = CLUSTER && live && !a.stats_in && !alone;
     if (tid == 0) {
       o.counted[it & 1] = live;
       if (meet) mbar_arrive_expect_tx(&o.got[meetings & 1], 8 * (g.cluster + (g.faulty(FAULT_SUMS, (int64_t)mine + it * clusters) && (int)rank == g.cluster - 1)));
@@ -451,7 +436,7 @@ __global__ void __launch_bounds__((LIGHT ? MAX_CONSUMERS : MAX_HOLDING) + 64, 1)
     bool loaded = true;
     if (weight != 0.f) {
       loaded = wait_loaded(&o.full[s], (phases >> s) & 1, g.polls);
-      if (!loaded) o.give_up = it + 1;
+      if (!loaded) lose(it);
       phases ^= 1u << s;
     }
     Raw<T, VE> raw[PIECES];
@@ -514,7 +499,10 @@ __global__ void __launch_bounds__((LIGHT ? MAX_CONSUMERS : MAX_HOLDING) + 64, 1)
       if (meet) {
         if (tid < g.cluster) push_pair(&o.all[meetings & 1][rank], &o.got[meetings & 1], (unsigned)tid, make_float2(M, S));
         __syncwarp();
-        if (!wait_pushed(&o.got[meetings & 1], (meetings >> 1) & 1, g.polls)) o.give_up = it + 1;
+        if (!__all_sync(0xffffffffu, wait_pushed(&o.got[meetings & 1], (meetings >> 1) & 1, g.polls))) {
+          alone = true;
+          lose(it);
+        }
         M = -INFINITY;
         S = 0.f;
         for (int c = 0; c < g.cluster; ++c) M = fmaxf(M, o.all[meetings & 1][c].x);
