@@ -144,18 +144,14 @@ __device__ __forceinline__ Raw<T, N> fetched(const uint8_t* from) {
   return load_raw<N>(reinterpret_cast<const T*>(from), N, true);
 }
 
-// Decay over a whole segment applied to a carried value; a zero stays one whatever the factor.  A factor near or past the type's range
-// is applied as its root, twice: the product may be a number all the same (a state that has all but faded and then grows, or
-// the other way round; its steps, one after the other, never leave the range).  256 units cover the whole of it.
-__device__ __forceinline__ float carry1(float up, float v, float end) {
-  const bool far = fabsf(up) > 120.f;
-  const float p = ex2(far ? 0.5f * up : up);
-  if (far) v *= p;
-  return v == 0.f ? end : fmaf(p, v, end);
-}
+// Decay over a whole segment applied to a carried value, as its root twice, since the factor may lie past the type's range where the
+// product does not (a state that has all but faded and then grows, or the other way round; step by step it never leaves the range).
+// A zero stays one whatever the factor.
 __device__ __forceinline__ pair carry2(pair A, float dts, pair v, pair end) {
-  const float2 p = unpack2(fma2(both(dts), A, both(kDecayUp))), x = unpack2(v), e = unpack2(end);
-  return pack2(carry1(p.x, x.x, e.x), carry1(p.y, x.y, e.y));
+  const float2 h = unpack2(fma2(both(0.5f * dts), A, both(kDecayUp)));
+  const pair root = pack2(ex2(h.x), ex2(h.y));
+  const float2 x = unpack2(v), r = unpack2(fma2(root, mul2(root, v), end)), e = unpack2(end);
+  return pack2(x.x == 0.f ? e.x : r.x, x.y == 0.f ? e.y : r.y);
 }
 // sum over a lane's states of x y
 __device__ __forceinline__ float dot(const pair (&x)[4], const pair (&y)[4]) {
