@@ -6,8 +6,11 @@ library and fails loudly when it has not been built -- there is no fallback.
 """
 from __future__ import annotations
 
+import array
 import ctypes as C
+import functools
 import os
+import struct
 
 import numpy as np
 
@@ -413,8 +416,8 @@ def mebptt_slot_copy(dst, src, nbytes: int, stream=None):
 
 
 # ---- operators over sequences ----------------------------------------------------------------------------------------
-# Arrays over time are torch tensors [t, batch, width], of any strides along t and batch: a descriptor holds those strides
-# (x.stride(0), x.stride(1)), so one descriptor serves all arrays that lie alike.
+# Arrays over time are torch tensors [t, batch, width], of any strides along t and batch and contiguous columns: a descriptor holds those
+# strides (x.stride(0), x.stride(1)), so one descriptor serves all arrays that lie alike.  All other tensors are contiguous.
 
 MEBPTT_CONV_SILU = 1
 MEBPTT_SCAN_SOFTPLUS = 1
@@ -440,43 +443,149 @@ def make_distill_desc(rows, vocabulary, entries, dtype, temperature=1.0, scale=1
     return mebptt_distill_desc(rows, vocabulary, entries, _dtype(dtype), 0, temperature, scale, logits_row, dlogits_row)
 
 
-_TYPES = {}
+# What a call takes a tensor for: (type, elements, lies dense, shape, strides).  Dense: contiguous and of as many elements at least, whatever
+# its shape.  Otherwise an array over time (or rows of logits) with gaps; `elements` is then how far its last one lies from its first.
+_torch = _describe = _places = None
+_NONE = id(None)
 
 
-def _pointers(name, desc, operands, floats, ints=()):
-    """Addresses of the tensors, in three lists.  Raises where one's type or place is not what the call takes it for (a wrong
-    one would be read past its end)."""
-    if not _TYPES:
+def _types(d):
+    """torch's types of operands, of everything float32, of whole numbers."""
+    global _torch, _describe, _places
+    if _torch is None:
         import torch
-        _TYPES.update({MEBPTT_BF16: torch.bfloat16, MEBPTT_FP32: torch.float32, MEBPTT_TF32: torch.float32, "f": torch.float32, "i": torch.int32})
-    out = []
-    for group, want in ((operands, _TYPES.get(desc.dtype)), (floats, _TYPES["f"]), (ints, _TYPES["i"])):
-        p = []
-        for x in group:
-            if x is None:
-                p.append(None)
-            elif x.dtype is want and x.is_cuda:
-                p.append(x.data_ptr())
-            else:
-                raise MebpttError(MEBPTT_ERR_ARG, f"{name}: a {x.dtype} tensor on {x.device} where a CUDA tensor of {want} belongs")
-        out.append(p)
-    return out
+        # the table of C functions of the DLPack specification: version, older table, allocator, two conversions, description
+        capsule = C.PYFUNCTYPE(_vp, C.py_object, C.c_char_p)(("PyCapsule_GetPointer", C.pythonapi))
+        table = (C.c_uint64 * 6).from_address(capsule(torch.Tensor.__dlpack_c_exchange_api__, b"dlpack_exchange_api"))
+        if table[0] & 0xffffffff != 1:
+            raise MebpttError(MEBPTT_ERR_UNSUPPORTED, "tensors: DLPack of another version than 1")
+        _describe = table[5]
+        _places = C.PyDLL(LIB_PATH).mebptt_binding_places      # (which keeps Python's lock)
+        _places.restype, _places.argtypes = _i32, [_vp, C.c_char_p, _vp, _i32, _i32, _vp]
+        _torch = torch
+    operand = {MEBPTT_BF16: _torch.bfloat16, MEBPTT_FP32: _torch.float32, MEBPTT_TF32: _torch.float32}.get(d.dtype)
+    return operand, _torch.float32, _torch.int32
+
+
+def _flat(dtype, n):
+    return dtype, n, True, None, None
+
+
+def _spread(dtype, shape, *strides):
+    """An array of this shape whose columns are contiguous; all strides 0: dense."""
+    dense, n = [], 1
+    for size in reversed(shape):
+        dense.insert(0, n)
+        n *= size
+    strides = (*strides, 1) if any(strides) else tuple(dense)
+    lies_dense = all(size <= 1 or a == b for size, a, b in zip(shape, strides, dense))
+    return dtype, 1 + sum((size - 1) * a for size, a in zip(shape, strides)), lies_dense, shape, strides
+
+
+def _packed(wants):
+    """The same as csrc/tensor_args.cpp reads it."""
+    code = {_torch.int32: (0, 32), _torch.float32: (2, 32), _torch.bfloat16: (4, 16)}
+    pad = lambda v: (*(v or ()), 0, 0, 0)[:3]  # noqa: E731
+    return b"".join(struct.pack("@iiqii3q3q", *code.get(e, (-1, 0)), n, dense, len(shape or ()), *pad(shape), *pad(strides))
+                    for e, n, dense, shape, strides in wants), wants
+
+
+@functools.lru_cache(256)
+def _conv_wants(raw):
+    d = mebptt_conv_desc.from_buffer_copy(raw)
+    e, f, i = _types(d)
+    x, y = (_spread(e, (d.t, d.batch, d.channels), *at) for at in ((d.x_step, d.x_row), (d.y_step, d.y_row)))
+    w, bias, state, n = d.channels * d.width, d.channels, _flat(e, d.batch * (d.width - 1) * d.channels), _flat(i, d.batch)
+    return (_packed((x, _flat(e, w), _flat(f, bias), state, n, y, state)),
+            _packed((x, _flat(e, w), _flat(f, bias), state, n, y, state, x, _flat(f, w), _flat(f, bias), state)))
+
+
+@functools.lru_cache(256)
+def _scan_wants(raw):
+    d = mebptt_scan_desc.from_buffer_copy(raw)
+    e, f, i = _types(d)
+    u, delta, z, y = (_spread(e, (d.t, d.batch, d.channels), *at) for at in ((d.u_step, d.u_row), (d.delta_step, d.delta_row),
+                                                                             (d.z_step, d.z_row), (d.y_step, d.y_row)))
+    b, c = (_spread(e, (d.t, d.batch, d.groups * d.states), *at) for at in ((d.b_step, d.b_row), (d.c_step, d.c_row)))
+    A, row, state, n = _flat(f, d.channels * d.states), _flat(f, d.channels), _flat(f, d.batch * d.channels * d.states), _flat(i, d.batch)
+    kept = lib.mebptt_scan_kept_bytes(C.addressof(d))
+    return (_packed((u, delta, A, b, c, row, z, row, state, n, y, state)),
+            _packed((u, delta, A, b, c, row, z, row, n, y, state, u, delta, A, b, c, row, z, row, state)), kept)
+
+
+@functools.lru_cache(256)
+def _distill_wants(raw):
+    d = mebptt_distill_desc.from_buffer_copy(raw)
+    e, f, i = _types(d)
+    x, dx = (_spread(e, (d.rows, d.vocabulary), row) for row in (d.logits_row, d.dlogits_row))
+    entries, one, rows, stats = d.rows * d.entries, _flat(f, 1), _flat(f, d.rows), _flat(f, 2 * d.rows)
+    teacher = x, _flat(i, entries), _flat(f, entries), rows
+    return _packed((*teacher, one, rows, stats)), _packed((*teacher, stats, one, dx)), _packed((*teacher, one, one, rows, dx))
+
+
+_DEVICE = -2                 # where tensors belong: the current CUDA device (-1: the host, for tests)
+
+
+def _addresses(name, wants, tensors):
+    """Addresses of the tensors.  Raises where one is not what the call takes it for: of another type, on another device than the
+    current one, or lying otherwise (its numbers would be others') or too short (it would be read or written past its end)."""
+    places = array.array("Q", map(id, tensors))
+    try:
+        if not _places(_describe, wants[0], places.buffer_info()[0], len(tensors), _DEVICE, _NONE):
+            return places.tolist()
+    except RuntimeError:                                          # not a tensor
+        pass
+    return [None if x is None else _lies_otherwise(name, x, dtype, n, shape, strides) for x, (dtype, n, _, shape, strides) in zip(tensors, wants[1])]
+
+
+def _here(x):
+    return x.is_cuda and x.get_device() == _torch.cuda.current_device() if _DEVICE == -2 else x.get_device() == _DEVICE
+
+
+def _refuse(name, what):
+    raise MebpttError(MEBPTT_ERR_ARG, f"{name}: {what}")
+
+
+def _lies_otherwise(name, x, dtype, n, shape, strides):
+    """The address of a tensor that has another shape than the array over time it is taken for, where that is right all the same (a
+    buffer that holds it); raises for all others."""
+    if x.dtype is not dtype:
+        _refuse(name, f"a {x.dtype} tensor on {x.device} where a CUDA tensor of {dtype} belongs")
+    sizes, at = tuple(x.shape), x.stride()
+    if shape is None:
+        if not x.is_contiguous():
+            _refuse(name, f"a tensor of strides {at} where a contiguous one belongs")
+        if x.numel() < n:
+            _refuse(name, f"a tensor of {x.numel()} elements where {n} belong")
+    else:
+        if sizes and sizes[-1] > 1 and at[-1] != 1:
+            _refuse(name, f"a tensor of strides {at}, whose columns are not contiguous")
+        if sizes == shape and any(size > 1 and a != b for size, a, b in zip(sizes, at, strides)):
+            _refuse(name, f"a tensor of strides {at} where the descriptor has {strides}")
+        reach = 1 + sum((size - 1) * a for size, a in zip(sizes, at)) if x.numel() else 0
+        if reach < n:
+            _refuse(name, f"a tensor that ends {reach} elements from its first where the descriptor's last is the {n}th")
+    if not _here(x):
+        _refuse(name, f"a tensor on {x.device} where one on the current CUDA device belongs")
+    return x.data_ptr()
 
 
 def _room(name, what, x, need):
     """Address and size of a buffer of bytes (0 for none); raises where it is smaller than the call takes it for."""
     if x is None:
         return None, 0
-    n = _nbytes(x)
+    n = x.numel() * x.element_size()
     if n < need:
         raise MebpttError(MEBPTT_ERR_WORKSPACE, f"{name}: {what}")
+    if not x.is_contiguous() or not _here(x):
+        raise MebpttError(MEBPTT_ERR_ARG, f"{name}: a {what} of strides {x.stride()} on {x.device} where a contiguous one on the current CUDA device belongs")
     return x.data_ptr(), n
 
 
 def mebptt_conv_forward(desc, x, w, bias, s_in, lengths, stream, y, s_out):
-    (x, w, s_in, y, s_out), (bias,), (lengths,) = _pointers("mebptt_conv_forward", desc, (x, w, s_in, y, s_out), (bias,), (lengths,))
-    st = lib.mebptt_conv_forward(C.addressof(desc), x, w, bias, s_in, lengths, stream, y, s_out)
-    _check(st, "mebptt_conv_forward")
+    name, raw = "mebptt_conv_forward", bytes(desc)
+    x, w, bias, s_in, lengths, y, s_out = _addresses(name, _conv_wants(raw)[0], (x, w, bias, s_in, lengths, y, s_out))
+    _check(lib.mebptt_conv_forward(raw, x, w, bias, s_in, lengths, stream, y, s_out), name)
 
 
 def mebptt_conv_workspace_bytes(desc) -> int:
@@ -484,11 +593,11 @@ def mebptt_conv_workspace_bytes(desc) -> int:
 
 
 def mebptt_conv_backward(desc, x, w, bias, s_in, lengths, dy, ds_out, workspace, stream, dx, dw, dbias, ds_in):
-    name = "mebptt_conv_backward"
-    (x, w, s_in, dy, ds_out, dx, ds_in), (bias, dw, dbias), (lengths,) = _pointers(
-        name, desc, (x, w, s_in, dy, ds_out, dx, ds_in), (bias, dw, dbias), (lengths,))
+    name, raw = "mebptt_conv_backward", bytes(desc)
+    x, w, bias, s_in, lengths, dy, ds_out, dx, dw, dbias, ds_in = _addresses(
+        name, _conv_wants(raw)[1], (x, w, bias, s_in, lengths, dy, ds_out, dx, dw, dbias, ds_in))
     ws, nbytes = _room(name, "workspace", workspace, 0)
-    _check(lib.mebptt_conv_backward(C.addressof(desc), x, w, bias, s_in, lengths, dy, ds_out, ws, nbytes, stream, dx, dw, dbias, ds_in), name)
+    _check(lib.mebptt_conv_backward(raw, x, w, bias, s_in, lengths, dy, ds_out, ws, nbytes, stream, dx, dw, dbias, ds_in), name)
 
 
 def mebptt_scan_kept_bytes(desc) -> int:
@@ -500,41 +609,43 @@ def mebptt_scan_workspace_bytes(desc, backward=False) -> int:
 
 
 def mebptt_scan_forward(desc, u, delta, A, Bm, Cm, skip, z, delta_bias, s_in, lengths, workspace, stream, y, s_out, kept=None):
-    name = "mebptt_scan_forward"
-    (u, delta, Bm, Cm, z, y), (A, skip, delta_bias, s_in, s_out), (lengths,) = _pointers(
-        name, desc, (u, delta, Bm, Cm, z, y), (A, skip, delta_bias, s_in, s_out), (lengths,))
+    name, raw = "mebptt_scan_forward", bytes(desc)
+    wants, _, room = _scan_wants(raw)
+    u, delta, A, Bm, Cm, skip, z, delta_bias, s_in, lengths, y, s_out = _addresses(
+        name, wants, (u, delta, A, Bm, Cm, skip, z, delta_bias, s_in, lengths, y, s_out))
     ws, nbytes = _room(name, "workspace", workspace, 0)
-    kept = None if kept is None else _room(name, "kept", kept, mebptt_scan_kept_bytes(desc))[0]
-    _check(lib.mebptt_scan_forward(C.addressof(desc), u, delta, A, Bm, Cm, skip, z, delta_bias, s_in, lengths, ws, nbytes, stream, y, s_out, kept), name)
+    kept = _room(name, "kept", kept, room)[0]
+    _check(lib.mebptt_scan_forward(raw, u, delta, A, Bm, Cm, skip, z, delta_bias, s_in, lengths, ws, nbytes, stream, y, s_out, kept), name)
 
 
 def mebptt_scan_backward(desc, u, delta, A, Bm, Cm, skip, z, delta_bias, lengths, kept, dy, ds_out, workspace, stream, du, ddelta,
                          dA, dB, dC, dskip, dz, ddelta_bias, ds_in):
-    name = "mebptt_scan_backward"
-    (u, delta, Bm, Cm, z, dy, du, ddelta, dB, dC, dz), (A, skip, delta_bias, ds_out, dA, dskip, ddelta_bias, ds_in), (lengths,) = _pointers(
-        name, desc, (u, delta, Bm, Cm, z, dy, du, ddelta, dB, dC, dz), (A, skip, delta_bias, ds_out, dA, dskip, ddelta_bias, ds_in), (lengths,))
+    name, raw = "mebptt_scan_backward", bytes(desc)
+    _, wants, room = _scan_wants(raw)
+    u, delta, A, Bm, Cm, skip, z, delta_bias, lengths, dy, ds_out, du, ddelta, dA, dB, dC, dskip, dz, ddelta_bias, ds_in = _addresses(
+        name, wants, (u, delta, A, Bm, Cm, skip, z, delta_bias, lengths, dy, ds_out, du, ddelta, dA, dB, dC, dskip, dz, ddelta_bias, ds_in))
     ws, nbytes = _room(name, "workspace", workspace, 0)
-    kept = None if kept is None else _room(name, "kept", kept, mebptt_scan_kept_bytes(desc))[0]
-    _check(lib.mebptt_scan_backward(C.addressof(desc), u, delta, A, Bm, Cm, skip, z, delta_bias, lengths, kept, dy, ds_out, ws, nbytes, stream,
+    kept = _room(name, "kept", kept, room)[0]
+    _check(lib.mebptt_scan_backward(raw, u, delta, A, Bm, Cm, skip, z, delta_bias, lengths, kept, dy, ds_out, ws, nbytes, stream,
                                     du, ddelta, dA, dB, dC, dskip, dz, ddelta_bias, ds_in), name)
 
 
 def mebptt_distill_loss(desc, logits, indices, values, weights, stream, loss, row_loss, row_stats):
-    name = "mebptt_distill_loss"
-    (logits,), (values, weights, loss, row_loss, row_stats), (indices,) = _pointers(
-        name, desc, (logits,), (values, weights, loss, row_loss, row_stats), (indices,))
-    _check(lib.mebptt_distill_loss(C.addressof(desc), logits, indices, values, weights, stream, loss, row_loss, row_stats), name)
+    name, raw = "mebptt_distill_loss", bytes(desc)
+    logits, indices, values, weights, loss, row_loss, row_stats = _addresses(
+        name, _distill_wants(raw)[0], (logits, indices, values, weights, loss, row_loss, row_stats))
+    _check(lib.mebptt_distill_loss(raw, logits, indices, values, weights, stream, loss, row_loss, row_stats), name)
 
 
 def mebptt_distill_grad(desc, logits, indices, values, weights, row_stats, dloss, stream, dlogits):
-    name = "mebptt_distill_grad"
-    (logits, dlogits), (values, weights, row_stats, dloss), (indices,) = _pointers(
-        name, desc, (logits, dlogits), (values, weights, row_stats, dloss), (indices,))
-    _check(lib.mebptt_distill_grad(C.addressof(desc), logits, indices, values, weights, row_stats, dloss, stream, dlogits), name)
+    name, raw = "mebptt_distill_grad", bytes(desc)
+    logits, indices, values, weights, row_stats, dloss, dlogits = _addresses(
+        name, _distill_wants(raw)[1], (logits, indices, values, weights, row_stats, dloss, dlogits))
+    _check(lib.mebptt_distill_grad(raw, logits, indices, values, weights, row_stats, dloss, stream, dlogits), name)
 
 
 def mebptt_distill_loss_grad(desc, logits, indices, values, weights, dloss, stream, loss, row_loss, dlogits):
-    name = "mebptt_distill_loss_grad"
-    (logits, dlogits), (values, weights, dloss, loss, row_loss), (indices,) = _pointers(
-        name, desc, (logits, dlogits), (values, weights, dloss, loss, row_loss), (indices,))
-    _check(lib.mebptt_distill_loss_grad(C.addressof(desc), logits, indices, values, weights, dloss, stream, loss, row_loss, dlogits), name)
+    name, raw = "mebptt_distill_loss_grad", bytes(desc)
+    logits, indices, values, weights, dloss, loss, row_loss, dlogits = _addresses(
+        name, _distill_wants(raw)[2], (logits, indices, values, weights, dloss, loss, row_loss, dlogits))
+    _check(lib.mebptt_distill_loss_grad(raw, logits, indices, values, weights, dloss, stream, loss, row_loss, dlogits), name)

@@ -152,3 +152,159 @@ def test_distill_refuses_temperatures_whose_square_is_not_a_normal_number(which)
         assert _distill(which, temperature=T) == B.MEBPTT_ERR_ARG, T
     for T in (1.1e-19, 1e-3, 1e4, 1.8e19):
         assert _distill(which, temperature=T, rows=1 << 31) == B.MEBPTT_ERR_UNSUPPORTED, T        # taken, but for the rows
+
+
+def _tensors(op, e="bf16", t=5, batch=3, D=8, W=4, S=16, G=2, rows=6, V=40, K=4):
+    """The tensors of each call."""
+    import torch
+    o = torch.bfloat16 if e == "bf16" else torch.float32
+    z = lambda *n, dtype=o: torch.zeros(*n, dtype=dtype)  # noqa: E731
+    f = lambda *n: z(*n, dtype=torch.float32)  # noqa: E731
+    i = lambda *n: z(*n, dtype=torch.int32)  # noqa: E731
+    if op.startswith("conv"):
+        d = B.make_conv_desc(batch, D, W, t, e)
+        a = dict(x=z(t, batch, D), w=z(D, W), bias=f(D), s_in=z(batch, W - 1, D), lengths=i(batch))
+        if op == "conv_forward":
+            return d, dict(**a, stream=None, y=z(t, batch, D), s_out=z(batch, W - 1, D))
+        return d, dict(**a, dy=z(t, batch, D), ds_out=z(batch, W - 1, D), workspace=None, stream=None, dx=z(t, batch, D), dw=f(D, W), dbias=f(D),
+                       ds_in=z(batch, W - 1, D))
+    if op.startswith("scan"):
+        d = B.make_scan_desc(batch, D, S, G, t, e)
+        a = dict(u=z(t, batch, D), delta=z(t, batch, D), A=f(D, S), Bm=z(t, batch, G * S), Cm=z(t, batch, G * S), skip=f(D), z=z(t, batch, D), delta_bias=f(D))
+        if op == "scan_forward":
+            return d, dict(**a, s_in=f(batch, D, S), lengths=i(batch), workspace=None, stream=None, y=z(t, batch, D), s_out=f(batch, D, S), kept=None)
+        return d, dict(**a, lengths=i(batch), kept=None, dy=z(t, batch, D), ds_out=f(batch, D, S), workspace=None, stream=None, du=z(t, batch, D),
+                       ddelta=z(t, batch, D), dA=f(D, S), dB=z(t, batch, G * S), dC=z(t, batch, G * S), dskip=f(D), dz=z(t, batch, D), ddelta_bias=f(D),
+                       ds_in=f(batch, D, S))
+    d = B.make_distill_desc(rows, V, K, e)
+    a = dict(logits=z(rows, V), indices=i(rows, K), values=f(rows, K), weights=f(rows))
+    if op == "distill_loss":
+        return d, dict(**a, stream=None, loss=f(1), row_loss=f(rows), row_stats=f(rows, 2))
+    if op == "distill_grad":
+        return d, dict(**a, row_stats=f(rows, 2), dloss=f(1), stream=None, dlogits=z(rows, V))
+    return d, dict(**a, dloss=f(1), stream=None, loss=f(1), row_loss=f(rows), dlogits=z(rows, V))
+
+
+OK = "taken"
+
+
+def _says(op, desc, kw):
+    """What the call is refused with, or OK."""
+    try:
+        getattr(B, "mebptt_" + op)(desc, **kw)
+    except B.MebpttError as e:
+        assert e.status == B.MEBPTT_ERR_ARG
+        return str(e)
+    return OK
+
+
+@pytest.fixture()
+def hosted(monkeypatch):
+    """The binding as it is where the host is the current device, with a library whose calls do nothing."""
+    class Library:
+        def __getattr__(self, name):
+            return real[name] if name.endswith("_bytes") or name == "mebptt_strerror" else lambda *a: B.MEBPTT_OK
+
+    real = {n: getattr(B.lib, n) for n in B._SIGS}
+    monkeypatch.setattr(B, "_DEVICE", -1)                                  # get_device() of a host tensor
+    monkeypatch.setattr(B, "lib", Library())
+
+
+CALLS = ["conv_forward", "conv_backward", "scan_forward", "scan_backward", "distill_loss", "distill_grad", "distill_loss_grad"]
+
+
+@pytest.mark.parametrize("e", ["bf16", "fp32"])
+@pytest.mark.parametrize("op", CALLS)
+def test_tensors_that_lie_otherwise_or_end_too_early_are_refused(hosted, op, e):
+    import torch
+    desc, right = _tensors(op, e)
+    assert _says(op, desc, right) == OK
+    for name, x in right.items():
+        if x is None:
+            continue
+        other = torch.float32 if x.dtype is not torch.float32 else torch.float64
+        assert f"a {other} tensor" in _says(op, desc, {**right, name: x.to(other)}), name
+        wide = torch.zeros(*x.shape[:-1], 2 * x.shape[-1], dtype=x.dtype)
+        if x.numel() > 1:
+            assert "strides" in _says(op, desc, {**right, name: wide[..., ::2]}), name              # every second column
+            assert "strides" in _says(op, desc, {**right, name: wide[:1, ..., :1].expand(x.shape) if x.dim() > 1 else wide[:1].expand(x.shape)}), name
+        if x.dim() > 1:
+            assert "strides" in _says(op, desc, {**right, name: x.transpose(-1, -2).contiguous().transpose(-1, -2)}), name
+            assert "strides" in _says(op, desc, {**right, name: wide[..., :x.shape[-1]]}), name      # a slice, where the descriptor has a dense array
+        assert "belong" in _says(op, desc, {**right, name: x.flatten()[:-1]}) or "ends" in _says(op, desc, {**right, name: x.flatten()[:-1]}), name
+        assert _says(op, desc, {**right, name: x.flatten()}) == OK, name                              # as many, in one dimension
+        assert _says(op, desc, {**right, name: torch.cat([x.flatten()] * 2)}) == OK, name
+
+
+def test_arrays_over_time_with_gaps_are_taken_as_the_descriptor_says(hosted):
+    import torch
+    t, N, D = 5, 3, 8
+    _, right = _tensors("conv_forward")
+    memory = torch.zeros(N, t, 2 * D, dtype=torch.bfloat16)
+    x = memory[:, :, :D].transpose(0, 1)                            # [t, N, D], batch-major, half of the columns
+    desc = B.make_conv_desc(N, D, 4, t, "bf16", x_strides=(x.stride(0), x.stride(1)))
+    assert _says("conv_forward", desc, {**right, "x": x}) == OK
+    assert _says("conv_forward", desc, {**right, "x": memory[:, :, :D]}) == OK      # the same places under other names
+    assert _says("conv_forward", desc, {**right, "x": memory}) == OK                # a buffer that holds them
+    assert "strides" in _says("conv_forward", desc, right)                          # a dense array is not what this descriptor says
+    assert "ends" in _says("conv_forward", desc, {**right, "x": memory.flatten()[:-D - 1]})
+    assert _says("conv_forward", desc, {**right, "x": memory.flatten()[:-D]}) == OK  # (nothing is read behind the last column)
+    assert "ends" in _says("conv_forward", desc, {**right, "x": x[:-1]})
+    assert "columns" in _says("conv_forward", desc, {**right, "x": memory.transpose(1, 2)})
+    # one step: rows of a wider array, with and without the dimension of time
+    one = B.make_conv_desc(N, D, 4, 1, "bf16", x_strides=(99, t * 2 * D), y_strides=(0, 0))
+    right["y"] = right["y"][:1]
+    for v in (x[:1], x[0], memory[:, 0], memory[:, 0, :D]):
+        assert _says("conv_forward", one, {**right, "x": v}) == OK
+    assert "ends" in _says("conv_forward", one, {**right, "x": x[0, :-1]})
+    # logits: rows with gaps
+    _, right = _tensors("distill_loss")
+    desc = B.make_distill_desc(6, 40, 4, "bf16", logits_row=48)
+    rows = torch.zeros(6, 48, dtype=torch.bfloat16)
+    for v in (rows, rows[:, :40], rows.view(2, 3, 48)[..., :40]):
+        assert _says("distill_loss", desc, {**right, "logits": v}) == OK
+    assert "strides" in _says("distill_loss", desc, right) and "ends" in _says("distill_loss", desc, {**right, "logits": rows[:5]})
+    # an optional tensor may be missing, and a width of one has no state
+    desc, right = _tensors("conv_forward", W=1)
+    assert _says("conv_forward", desc, {**right, "bias": None, "lengths": None, "s_in": None, "s_out": None}) == OK
+
+
+def test_tensors_of_another_device_than_the_current_one_are_refused(hosted, monkeypatch):
+    import torch
+
+    class On:
+        """A tensor as if it were on a CUDA device."""
+        def __init__(self, x, device):
+            self.x, self.device_at = x, device
+
+        def __getattr__(self, k):
+            return getattr(self.x, k)
+
+        is_cuda = True
+
+        def get_device(self):
+            return self.device_at
+
+    for op in CALLS:
+        desc, right = _tensors(op)
+        monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+        monkeypatch.setattr(B, "_DEVICE", -2)
+        assert "current CUDA device" in _says(op, desc, right)              # host tensors
+        here = {k: v if v is None else On(v, 0) for k, v in right.items()}
+        assert _says(op, desc, here) == OK
+        for name, x in right.items():
+            if x is not None:
+                assert "current CUDA device" in _says(op, desc, {**here, name: On(x, 1)}), name
+                assert "current CUDA device" in _says(op, desc, {**here, name: x}), name
+
+
+def test_rooms_are_contiguous_and_on_the_current_device(hosted):
+    import torch
+    desc, right = _tensors("scan_backward")
+    room = torch.zeros(2, B.mebptt_scan_kept_bytes(desc), dtype=torch.uint8)
+    for name in ("kept", "workspace"):
+        assert _says("scan_backward", desc, {**right, name: room[0]}) == OK
+        assert "contiguous" in _says("scan_backward", desc, {**right, name: room.t()}), name
+    with pytest.raises(B.MebpttError) as e:
+        B.mebptt_scan_backward(desc, **{**right, "kept": room[0, :-1]})
+    assert e.value.status == B.MEBPTT_ERR_WORKSPACE
