@@ -1,6 +1,5 @@
 // Distillation from a teacher's top logits: entry points, and the kernel for what the rings (distill_ring.cu) do not take -- gradients that
-// lie otherwise within 16 bytes than the logits, more than 128 entries at fewer than 2048 logits, rows longer than a cluster's
-// shared memory.
+// lie otherwise within 16 bytes than the logits, and rows longer than a cluster's shared memory.
 //
 // A row is held in the registers of a block of 32 to 512 threads, or of a cluster of up to eight blocks (up to 131072 logits): each
 // thread loads all its 16-byte pieces at once, takes their maximum m, turns them into exp((x - m) / T), and what remains once

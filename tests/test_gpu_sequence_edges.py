@@ -217,3 +217,42 @@ def test_distill_waits_that_run_out_show_in_every_output(fault, dtype, R, V, blo
     again = [v.clone() for v in (p.loss, p.row_loss, p.DX)]
     p.apart()
     assert all(_same(a, b) for a, b in zip(again, (p.loss, p.row_loss, p.DX))) and not bool(p.DX.isnan().any())
+
+
+def _fused_and_apart(p):
+    p.upload()
+    p.both()
+    p.check()
+    p.DX.fill_(7.0)
+    p.apart()
+    p.check()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("V,K", [(1, 129), (300, 1024), (1000, 200), (2040, 130), (2049, 1024)])
+def test_distill_more_entries_than_a_warp_takes_of_short_rows(dtype, V, K):
+    """Blocks of as few as one warp that computes, with many times as many entries: tokens of their own, a few of them again and again, none."""
+    p = Distill(dtype, 7, V, K, T=1.7, pad=3, phase=1)
+    r = np.random.default_rng(K)
+    p.i[1] = r.integers(0, V, K)
+    p.i[2] = r.integers(0, min(V, 5), K)
+    p.i[3, K // 3:] = -1
+    p.i[4] = -1
+    p.v[5, ::2] = -np.inf
+    p.w[6] = 0
+    _fused_and_apart(p)
+
+
+@pytest.mark.parametrize("dtype,V,other", [("bf16", 140001, True), ("fp32", 140001, True), ("bf16", 300000, True), ("bf16", 600001, False), ("fp32", 260000, False)])
+def test_distill_rows_that_no_ring_takes_and_no_registers_hold(dtype, V, other):
+    """Rows that are read a second time for the gradient: too long for a cluster's shared memory, or for its registers where the gradient
+    lies otherwise within 16 bytes than the logits."""
+    p = Distill(dtype, 3, V, 20, T=0.8, pad=5, phase=1)
+    if other:
+        row = V + 2
+        p.dmemory = torch.full((3 + 3 * row,), 977.0, device="cuda").to(p.X.dtype)
+        p.DX = p.dmemory.as_strided((3, V), (row, 1), 3)
+        p.row, p.desc.dlogits_row = row, row
+    p.i[1, 4:9] = p.i[1, 3]
+    p.w[2] = 0
+    _fused_and_apart(p)
