@@ -305,7 +305,9 @@ cudaError_t launch(const DistillArgs& a, int64_t rows, int cluster, int threads,
   at[0].val.clusterDim.x = (unsigned)cluster; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
   cfg.attrs = at;
   cfg.numAttrs = cluster > 1 ? 1 : 0;
-  return cluster > 1 ? cudaLaunchKernelEx(&cfg, distill_kernel<T, WHOLE, true>, a) : cudaLaunchKernelEx(&cfg, distill_kernel<T, WHOLE, false>, a);
+  if constexpr (WHOLE)
+    if (cluster == 1) return cudaLaunchKernelEx(&cfg, distill_kernel<T, true, false>, a);
+  return cudaLaunchKernelEx(&cfg, distill_kernel<T, WHOLE, true>, a);      // (rows that are read twice have passed a cluster of the largest size)
 }
 
 int finish(cudaError_t st, const DistillArgs& a, const mebptt_distill_desc* d, float* loss, cudaStream_t s) {

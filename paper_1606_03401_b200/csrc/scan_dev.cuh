@@ -40,7 +40,7 @@ __device__ __forceinline__ void store_pair(float* row, int n0, int states, bool 
   if (n0 < states) row[n0] = f.x;
   if (n0 + 1 < states) row[n0 + 1] = f.y;
 }
-// A lane's states out of a row of `states` values (zeros past the last), and back: in their own order, and in a lane's.
+// A lane's states out of a row of `states` values (zeros past the last), and back.
 __device__ __forceinline__ void load_states(const float* row, int l, int states, bool vec, pair (&s)[4]) {
   if (vec && PER_LANE * (l + 1) <= states) {
     const ulonglong2* const p = reinterpret_cast<const ulonglong2*>(row + PER_LANE * l);
@@ -60,14 +60,6 @@ __device__ __forceinline__ void store_states(float* row, int l, int states, bool
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i) store_pair(row, PER_LANE * l + 2 * i, states, vec, s[i]);
-}
-__device__ __forceinline__ void load_states(const float* row, int l, int turn, int states, bool vec, pair (&s)[4]) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) s[i] = load_pair(row, PER_LANE * l + pair_at(i, turn), states, vec);
-}
-__device__ __forceinline__ void store_states(float* row, int l, int turn, int states, bool vec, const pair (&s)[4]) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) store_pair(row, PER_LANE * l + pair_at(i, turn), states, vec, s[i]);
 }
 
 // Where (channel, step) of a tile lies in shared memory: steps of a channel together, so that a lane loads four at once, and groups of

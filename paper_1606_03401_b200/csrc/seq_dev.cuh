@@ -116,7 +116,6 @@ __device__ __forceinline__ float rcp(float x) {
   return y;
 }
 __device__ __forceinline__ float sigmoid(float x) { return rcp(1.f + ex2(-kLog2e * x)); }
-__device__ __forceinline__ float dsilu(float x, float sig) { return sig * (1.f + x * (1.f - sig)); }
 
 // log(1 + e^x) = max(x, 0) + log1p(e^{-|x|}), and log1p(e) = 2 atanh(e / (2 + e)) by its series: the argument is at most 1/3, so
 // eight terms leave 2e-9 of the value, and a small e keeps its relative precision.
