@@ -117,16 +117,11 @@ __device__ __forceinline__ float warp_sum(float v) {
   return v;
 }
 
-// Waits that a test lets run out (0: none), each at row `fault_row`.
-enum Fault { FAULT_LOAD = 1, FAULT_SUMS = 2, FAULT_LOSS = 4 };
-
 struct RingArgs {
   DistillArgs a;
   int cluster, stages, consumers, share;          // share: pieces of a block at most
-  int fault;
   uint32_t polls;                                 // of a wait
-  int64_t fault_row;
-  __device__ bool faulty(int kind, int64_t row) const { return (fault & kind) && row == fault_row; }
+  int64_t no_load, no_sums, no_loss;              // rows whose logits, sums of blocks, parts of a loss a test waits for in vain (-1: none)
 };
 
 // A row after a wait has run out, by a whole warp: loss, statistics (`tell`) and the gradient's elements from + first, from + first + by, ... below
@@ -240,7 +235,7 @@ __global__ void __launch_bounds__((LIGHT ? MAX_CONSUMERS : MAX_HOLDING) + 64, 1)
       T* const buf = (T*)stage(s);
       if (lane == 0) {
         const uint32_t bytes = (uint32_t)(w.in1 - w.in0) * 16;
-        const bool faulty = g.faulty(FAULT_LOAD, (int64_t)mine + it * clusters) && (int)rank == g.cluster - 1;
+        const bool faulty = (int64_t)mine + it * clusters == g.no_load && (int)rank == g.cluster - 1;
         mbar_arrive_expect_tx(&o.full[s], bytes + (faulty ? 16 : 0));
         if (bytes) bulk_in(buf + (w.in0 - w.p0) * VE, w.x + ((int64_t)w.in0 * VE - w.phase), bytes, &o.full[s]);
       }
@@ -387,7 +382,7 @@ __global__ void __launch_bounds__((LIGHT ? MAX_CONSUMERS : MAX_HOLDING) + 64, 1)
         if (lane == 0) {
           due = CLUSTER && o.counted[was & 1];
           if (due) {
-            if (rank == 0) mbar_arrive_expect_tx(&o.lost[losses & 1], 8 * (g.cluster + g.faulty(FAULT_LOSS, (int64_t)mine + was * clusters)));
+            if (rank == 0) mbar_arrive_expect_tx(&o.lost[losses & 1], 8 * (g.cluster + ((int64_t)mine + was * clusters == g.no_loss)));
             push_pair(&o.part[losses & 1][rank], &o.lost[losses & 1], 0, make_float2(v, 0.f));
           } else if (rank == 0) {
             a.row_loss[(int64_t)mine + was * clusters] = v;
@@ -433,7 +428,7 @@ __global__ void __launch_bounds__((LIGHT ? MAX_CONSUMERS : MAX_HOLDING) + 64, 1)
     const bool meet = CLUSTER && live && !a.stats_in && !alone;
     if (tid == 0) {
       o.counted[it & 1] = live;
-      if (meet) mbar_arrive_expect_tx(&o.got[meetings & 1], 8 * (g.cluster + (g.faulty(FAULT_SUMS, (int64_t)mine + it * clusters) && (int)rank == g.cluster - 1)));
+      if (meet) mbar_arrive_expect_tx(&o.got[meetings & 1], 8 * (g.cluster + ((int64_t)mine + it * clusters == g.no_sums && (int)rank == g.cluster - 1)));
     }
     T* const buf = (T*)stage(s);
     const Row w = row_at(it);
@@ -576,6 +571,17 @@ __global__ void __launch_bounds__((LIGHT ? MAX_CONSUMERS : MAX_HOLDING) + 64, 1)
   }
 }
 
+// What is left of a warp's rows after a wait has run out: the loads of this row and those ahead once more, then all from here on are lost.
+template <class T>
+__device__ __noinline__ void lost_rows(const RingArgs& g, uint64_t* full, int s, uint32_t phases, int64_t r, int64_t step) {
+  for (int i = 0; i < g.stages - 1; ++i) {
+    const int at = (s + i) % g.stages;
+    const int64_t row = r + i * step;
+    if (row < g.a.rows && !(g.a.weights && g.a.weights[row] == 0.f)) wait_loaded(&full[at], (phases >> at) & 1, g.polls);
+  }
+  for (; r < g.a.rows; r += step) lost_row<T>(g.a, r, 0, g.a.vocabulary, threadIdx.x % 32, 32, threadIdx.x % 32 == 0);
+}
+
 // Short rows: a warp each, with a ring of its own, so that nothing waits for another warp.  `share` pieces a row at most.
 constexpr int WARPS = 4, ENTRIES = 128;
 template <class T, int PIECES>
@@ -620,7 +626,7 @@ __global__ void __launch_bounds__(WARPS * 32, PIECES * 16 / (int)sizeof(T) == 32
     T* const buf = (T*)(ring + s * stage_bytes);
     if (lane == 0) {
       const uint32_t bytes = (uint32_t)(w.in1 - w.in0) * 16;
-      mbar_arrive_expect_tx(&full[s], bytes + (g.faulty(FAULT_LOAD, r) ? 16 : 0));
+      mbar_arrive_expect_tx(&full[s], bytes + (r == g.no_load ? 16 : 0));
       if (bytes) bulk_in(buf + w.in0 * VE, w.x + (w.in0 * VE - w.phase), bytes, &full[s]);
     }
     const int head = w.in0 * VE, tail = (w.pieces - w.in1) * VE;
@@ -828,14 +834,7 @@ __global__ void __launch_bounds__(WARPS * 32, PIECES * 16 / (int)sizeof(T) == 32
     __syncwarp();
   }
   if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
-  if (r < a.rows) {
-    // a wait has run out: the loads of this row and those ahead once more, then its rows from here on are lost
-    for (int i = 0; i < NS - 1; ++i) {
-      const int at = (s + i) % NS;
-      if (weight_of(r + i * step) != 0.f && r + i * step < a.rows) wait_loaded(&full[at], (phases >> at) & 1, g.polls);
-    }
-    for (; r < a.rows; r += step) lost_row<T>(a, r, 0, V, lane, 32, lane == 0);
-  }
+  if (r < a.rows) lost_rows<T>(g, full, s, phases, r, step);
 }
 
 size_t small_bytes(int share, int VE, int entries) {
@@ -921,9 +920,10 @@ bool distill_ring(const DistillArgs& a, bool half, cudaStream_t s, cudaError_t& 
   RingArgs g = {};
   g.a = a;
   const int fault = tc::wait_fault_mask() >> 5;      // testing aid, 0 outside the tests of the bounded waits
-  g.fault = fault;
   g.polls = fault ? tc::fault_poll_limit : kSpinLimit;
-  g.fault_row = a.rows / 2;
+  g.no_load = fault & 1 ? a.rows / 2 : -1;
+  g.no_sums = fault & 2 ? a.rows / 2 : -1;
+  g.no_loss = fault & 4 ? a.rows / 2 : -1;
   if (pieces * VE <= 2048 && a.entries <= ENTRIES) {
     g.share = (int)pieces;
     st = half ? launch_warps<bf16>(g, sms, s) : launch_warps<float>(g, sms, s);
