@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from paper_1606_03401_b200 import binding as B
-from tests.test_gpu_sequence_ops import Conv, Distill, _stream
+from tests.test_gpu_sequence_ops import Conv, Distill, Scan, _stream
 
 pytestmark = pytest.mark.gpu
 
@@ -274,3 +274,33 @@ def test_scan_decays_have_no_bias_where_states_last_for_thousands_of_steps(low, 
     assert abs(float(error.mean())) < 2.0 ** -24
     # argument (its two roundings), function and the product with the state, as the oracle counts them
     assert float((error.abs() - (2 * x.double() + 5) * 2.0 ** -24).max()) <= 0
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("V", [40, 3001, 50257, 140000, 600001])
+def test_distill_gradient_over_the_logits_in_every_kernel(dtype, V):
+    p = Distill(dtype, 4, V, 12, T=1.2, pad=7, phase=1)
+    p.DX, p.dmemory = p.X, p.memory
+    p.w[2] = 0
+    p.upload()
+    p.both()
+    p.check()
+    p.upload()
+    B.mebptt_distill_loss(p.desc, p.X, *p.dev, _stream(), p.loss, p.row_loss, p.stats)
+    B.mebptt_distill_grad(p.desc, p.X, *p.dev, p.stats, p.dloss, _stream(), p.X)
+    p.check()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("t,spacing", [(1, 8), (50, 8), (50, 32), (300, 16)])
+def test_scan_state_of_a_row_without_steps_is_handed_on_and_nothing_else(dtype, t, spacing):
+    a, b = (Scan(dtype, 5, t, 24, 16, spacing=spacing, seed=4) for _ in range(2))
+    empty = [r for r in range(5) if a.lengths[r] == 0]
+    assert empty
+    for p, v in ((a, 0.0), (b, float("nan"))):
+        p.dev["s_in"][empty] = v
+        p.forward()
+        p.backward()
+    assert bool(b.s_out[empty].isnan().all()) and torch.equal(b.ds_in[empty], b.dev["ds_out"][empty])
+    b.s_out[empty] = a.s_out[empty]
+    assert all(torch.equal(x, y) for x, y in zip(a.outputs(), b.outputs()))
