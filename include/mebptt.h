@@ -499,9 +499,10 @@ int mebptt_gemm_bf16(const void *A, int64_t lda, int a_major, const void *B, int
  *     s_out, ds_in (nullable) that of s_in.
  *   - Outputs are overwritten, not accumulated, and apart from s_out none may overlap an input.
  *     No atomics: the same inputs give the same bits.
- *   - Kernels only, on `stream` alone (a stream of the current device), with nothing allocated and
- *     nothing kept between calls: every call can be captured into a graph.  Calls whose work may
- *     overlap need workspaces of their own, two captured graphs too.
+ *   - Kernels only, on `stream` alone (a stream of the current device), with nothing allocated and no
+ *     data kept between calls: every call can be captured into a graph, and host threads may call at
+ *     once.  (Kept is how many clusters of a shape a device holds.)  Calls whose work may overlap need
+ *     workspaces of their own, two captured graphs too.
  *   - MEBPTT_ERR_UNSUPPORTED where a size passes what a grid or 32 bits can count (batch > 65535 or
  *     2^24 groups of more than 32 states backward for the scan, 2^31 rows of logits).
  */

@@ -8,11 +8,13 @@
 // the listed tokens are put right there, and the stage is copied out.  One warp moves data, another prepares the next row's teacher
 // (softmax of the listed values, tokens listed twice) and adds up losses.  Row begins and ends that are not on 16-byte
 // boundaries go by plain loads and stores of the first one.
-// Measured, loss and gradient in bfloat16: 4096 rows of 32000 in 102 us (5.2 TB/s), 16384 of 8192 in 100 us, 2048 of 50257 in 97 us
-// (4.2 TB/s), 512 of 128256 (clusters of four) in 72 us (3.6 TB/s; a row's path of 4 us is longer than its bytes take).
+// Measured, loss and gradient in bfloat16 with 64 listed tokens a row: 4096 rows of 32000 in 100 us (5.2 TB/s), 16384 of 8192 in 112 us
+// (4.8 TB/s), 2048 of 50257 in 100 us (4.1 TB/s), 512 of 128256 (clusters of four) in 74 us (3.6 TB/s; a row's path of 4 us is longer than
+// its bytes take).  The loss alone takes 81, 88, 66 and 62 us, the gradient from statistics 115, 117, 107 and 68.
 //
 // Up to 2048 logits and 128 entries: a warp has a row and a ring to itself, so that nothing waits for another warp.  65536 rows of 1024:
-// 100 us (2.7 TB/s; instructions for the 64 listed tokens of each row are half of it).
+// 105 us (2.6 TB/s; instructions for the 64 listed tokens of each row are half of it; 124 to 132 bytes a thread are spilt).  Rows that list a
+// token twice take a search over all pairs of entries on top: 532 us where nearly all do.
 //
 // Every wait is bounded (none runs out while the device works).  A block in which one has run out loads no more rows, since a barrier
 // must not be armed a second time before its phase is over, and neither pushes nor waits for what the cluster exchanges there:
