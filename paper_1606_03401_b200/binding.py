@@ -546,9 +546,20 @@ def _refuse(name, what):
     raise MebpttError(MEBPTT_ERR_ARG, f"{name}: {what}")
 
 
+def _walk(sizes, strides):
+    """The places of an array, whatever its dimensions are called: those of one step left out, those that continue one another joined."""
+    out = []
+    for size, a in sorted(((n, a) for n, a in zip(sizes, strides) if n > 1), key=lambda v: -v[1]):
+        if out and out[-1][1] == size * a:
+            out[-1] = (out[-1][0] * size, a)
+        else:
+            out.append((size, a))
+    return out
+
+
 def _lies_otherwise(name, x, dtype, n, shape, strides):
-    """The address of a tensor that has another shape than the array over time it is taken for, where that is right all the same (a
-    buffer that holds it); raises for all others."""
+    """The address of a tensor that has another shape than the array over time it is taken for, where that is right all the same: a
+    longer or wider array of these strides, the same rows in other dimensions, a contiguous buffer that holds it.  Raises for all others."""
     if x.dtype is not dtype:
         _refuse(name, f"a {x.dtype} tensor on {x.device} where a CUDA tensor of {dtype} belongs")
     sizes, at = tuple(x.shape), x.stride()
@@ -560,11 +571,16 @@ def _lies_otherwise(name, x, dtype, n, shape, strides):
     else:
         if sizes and sizes[-1] > 1 and at[-1] != 1:
             _refuse(name, f"a tensor of strides {at}, whose columns are not contiguous")
-        if sizes == shape and any(size > 1 and a != b for size, a, b in zip(sizes, at, strides)):
-            _refuse(name, f"a tensor of strides {at} where the descriptor has {strides}")
+        lies = f"a tensor of shape {sizes} and strides {at} where the descriptor has {shape} and {strides}"
+        longer = len(sizes) == len(shape) and all(a >= b for a, b in zip(sizes, shape)) and all(b <= 1 or a == c for a, b, c in zip(at, shape, strides))
+        if sizes == shape and not longer:
+            _refuse(name, lies)
         reach = 1 + sum((size - 1) * a for size, a in zip(sizes, at)) if x.numel() else 0
         if reach < n:
             _refuse(name, f"a tensor that ends {reach} elements from its first where the descriptor's last is the {n}th")
+        rows = sizes and sizes[-1] >= shape[-1] and _walk(sizes[:-1], at[:-1]) == _walk(shape[:-1], strides[:-1])
+        if not (longer or rows or x.is_contiguous()):
+            _refuse(name, lies)
     if not _here(x):
         _refuse(name, f"a tensor on {x.device} where one on the current CUDA device belongs")
     return x.data_ptr()

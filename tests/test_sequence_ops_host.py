@@ -251,6 +251,16 @@ def test_arrays_over_time_with_gaps_are_taken_as_the_descriptor_says(hosted):
     assert _says("conv_forward", desc, {**right, "x": memory.flatten()[:-D]}) == OK  # (nothing is read behind the last column)
     assert "ends" in _says("conv_forward", desc, {**right, "x": x[:-1]})
     assert "columns" in _says("conv_forward", desc, {**right, "x": memory.transpose(1, 2)})
+    # rows in one dimension, a longer array; gaps that the descriptor does not have, or has otherwise
+    wide = torch.zeros(t + 2, N, 2 * D, dtype=torch.bfloat16)
+    gaps = B.make_conv_desc(N, D, 4, t, "bf16", x_strides=(wide.stride(0), wide.stride(1)))
+    for v in (wide[:t, :, :D], wide[:, :, :D], wide.view(-1, 2 * D)[:t * N, :D], wide):
+        assert _says("conv_forward", gaps, {**right, "x": v}) == OK
+    dense = B.make_conv_desc(N, D, 4, t, "bf16")
+    for v in (wide.view(-1, 2 * D)[:, :D], wide[:, :, :D], wide[:, 0, :D]):
+        assert "strides" in _says("conv_forward", dense, {**right, "x": v})
+    assert "strides" in _says("conv_forward", gaps, {**right, "x": torch.zeros(t * N, 3 * D, dtype=torch.bfloat16)[:, :D]})
+    assert _says("conv_forward", gaps, {**right, "x": memory[:, :, :D]}) == OK      # (the same rows: which is which the descriptor says)
     # one step: rows of a wider array, with and without the dimension of time
     one = B.make_conv_desc(N, D, 4, 1, "bf16", x_strides=(99, t * 2 * D), y_strides=(0, 0))
     right["y"] = right["y"][:1]
